@@ -175,14 +175,14 @@ __device__ __forceinline__ Outcome outcome_of(const PolicyArgs& a, MaxSum all, f
     if (a.old_logp) {
         const float ratio = expf((float)(logp - (double)head.old_logp)), straight = ratio * head.adv;
         const float clipped = fminf(fmaxf(ratio, 1.f - a.lo), 1.f + a.hi) * head.adv;
-        token = -(straight <= clipped ? straight : clipped);
-        coef = straight <= clipped ? -straight : 0.f;
+        const bool taken = !(straight > clipped);                // also where a side is NaN, which the bounds would drop
+        token = -(taken ? straight : clipped);
+        coef = taken ? -straight : 0.f;
         if (a.ref) {
             const float gap = (float)((double)head.ref - logp), e = expm1f(gap);
             token = fmaf(a.beta, e - gap, token);
             coef = fmaf(-a.beta, e, coef);
         }
-        if (logp != logp) token = coef = nan;
         token *= w;
         coef *= w * a.inv_t;
     }

@@ -1,0 +1,56 @@
+"""Values at which the operators that make a worker's gradient could go wrong: NaN and infinities where they must come
+through, the ends of a type's range, padding, row shapes between the usual ones, and bounds that hold their precision."""
+import math
+
+import pytest
+import torch
+
+from paper_1905_10936_b200 import ops
+from test_ops_gpu import policy64, policy_case, within
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- policy loss -----------------------------------------------------------------------------
+SPECIAL = [(name, value) for name in ("old", "adv", "ref") for value in (math.nan, math.inf, -math.inf)]
+
+
+@pytest.mark.parametrize("with_ref", [True, False], ids=["kl", "no kl"])
+@pytest.mark.parametrize("n,c", [(40, 300), (320, 4000), (40, 20000)])
+def test_policy_loss_passes_on_what_is_not_finite(n, c, with_ref):
+    """NaN and infinities among a live row's scalars reach its loss and gradient as in the formulas (a NaN on either side of
+    the minimum is the minimum), and no other row's.  Rows of one warp, of four, of eight."""
+    lo, hi, beta = 0.2, 0.28, 0.1
+    x, t, old, adv, w, ref = policy_case(c, n, c, torch.float32, masked=0.0)
+    x[x == -math.inf] = -9.0
+    use = dict(clip_low=lo, clip_high=hi, beta=beta)
+    good = ops.policy_loss(x, t, old, adv, w, ref_logp=ref if with_ref else None, **use)
+    v = {"old": old.clone(), "adv": adv.clone(), "ref": ref.clone()}
+    special = SPECIAL if with_ref else SPECIAL[:6]
+    for i, (name, value) in enumerate(special):
+        v[name][3 * i] = value
+    i = 3 * len(special)                                          # a target of probability 0 that the old policy never gave either
+    x2 = x.clone()
+    x2[i, t[i]] = -math.inf
+    v["old"][i] = -math.inf
+    v["adv"][i + 1] = 0.0                                         # an infinite ratio times nothing
+    v["old"][i + 1] = -math.inf
+    out = ops.policy_loss(x2, t, v["old"], v["adv"], w, ref_logp=v["ref"] if with_ref else None, **use)
+    e = policy64(x2, t, v["old"], v["adv"], w, v["ref"] if with_ref else None, lo, hi, beta, 1.0)
+    coef = torch.where(e["straight"].isnan() | e["lp"].isnan(), torch.full_like(e["coef"], math.nan), e["coef"])
+    special_rows = torch.zeros(n, dtype=torch.bool, device="cuda")
+    special_rows[[3 * k for k in range(len(special) + 1)] + [i + 1]] = True
+    assert torch.equal(out.grad[~special_rows], good.grad[~special_rows])
+    assert torch.equal(out.token_loss[~special_rows], good.token_loss[~special_rows])
+    tok = e["tok"]
+    for k in special_rows.nonzero().view(-1).tolist():
+        assert bool(tok[k].isnan() == out.token_loss[k].isnan()) and bool(tok[k].isinf() == out.token_loss[k].isinf()), k
+        if bool(coef[k].isnan()):
+            assert bool(out.grad[k].isnan().all()), k
+        elif bool(coef[k].isinf()):
+            assert not bool(out.grad[k].isfinite().any()), k
+        else:
+            want = -coef[k] * e["p"][k]
+            want[t[k]] += coef[k]
+            within(out.grad[k], want, 1e-5 * coef[k].abs() + 1e-37, f"grad of row {k}")
+    assert bool(out.loss.isnan())
