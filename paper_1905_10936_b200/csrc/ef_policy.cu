@@ -236,6 +236,7 @@ __global__ void __launch_bounds__(Shape<GW>::kBlock, Shape<GW>::kCtas) ef_policy
         if (tid == 0) {
             T* const row = reinterpret_cast<T*>(slots + slot * slot_size + sl.phase);
             const int per = per_chunk_of(sl.vecs);
+            efk::fence_proxy_async();                            // the slot was last read through ordinary loads
             for (int c = 0, at = 0; at < sl.vecs; ++c, at += per) {
                 const unsigned bytes = (unsigned)min(per, sl.vecs - at) * 16u;
                 efk::mbar_expect_tx(&s_bar[group][slot][c], bytes);
@@ -410,11 +411,6 @@ __device__ __forceinline__ int taken_cta(const uint4* answer) {
                  : "=r"(v) : "r"(efk::smem_u32(answer)) : "memory");
     return v;
 }
-// An arrival without release: what it reports is reads of shared memory whose values have been used, and a release would
-// wait for the gradient's stores in flight.
-__device__ __forceinline__ void mbar_arrive_relaxed(unsigned long long* bar) {
-    asm volatile("mbarrier.arrive.relaxed.cta.shared::cta.b64 _, [%0];" ::"r"(efk::smem_u32(bar)) : "memory");
-}
 __device__ __forceinline__ void mbar_arrive(unsigned long long* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(efk::smem_u32(bar)) : "memory");
 }
@@ -470,6 +466,7 @@ __global__ void __launch_bounds__(kRowsThreads, 3) ef_policy_rows_kernel(const P
                     const bool free = c >= used || efk::mbar_wait_bounded(&s_free[c], freed >> c & 1u);
                     if (free && c < chunks && lane == 0) {
                         const unsigned bytes = (unsigned)min(per, sl.vecs - c * per) * 16u;
+                        efk::fence_proxy_async();                // the chunk was last read through ordinary loads
                         efk::mbar_expect_tx(&s_full[c], bytes);
                         efk::bulk_load(s_rows + c * per * 16, sl.x + sl.head + c * per * V, bytes, &s_full[c]);
                     }
@@ -500,9 +497,14 @@ __global__ void __launch_bounds__(kRowsThreads, 3) ef_policy_rows_kernel(const P
                 if (used != 0) load();
                 used = chunks;
             }
-            if (lane == 0) ask_for_cta(&s_answer, &s_answered);
+            if (lane == 0) {
+                efk::fence_proxy_async();                        // the last answer was read through an ordinary load, by this lane
+                ask_for_cta(&s_answer, &s_answered);
+            }
             ok = efk::mbar_wait_bounded(&s_answered, it & 1);
-            const int cta = ok ? taken_cta(&s_answer) : -1;
+            int cta = -1;
+            if (ok && lane == 0) cta = taken_cta(&s_answer);
+            cta = __shfl_sync(kFull, cta, 0);
             n = cta < 0 ? a.n : cta;
         }
         return;
@@ -530,7 +532,7 @@ __global__ void __launch_bounds__(kRowsThreads, 3) ef_policy_rows_kernel(const P
         const int edge = tid >= ends ? -1 : tid < sl.head ? tid : sl.tail + (tid - sl.head);
         const T edge_value = row.edge[tid & (2 * V - 1)];
         __syncwarp();
-        if (lane == 0) mbar_arrive_relaxed(&s_read[it & 1]);
+        if (lane == 0) mbar_arrive(&s_read[it & 1]);
         T* const g = a.grad ? static_cast<T*>(a.grad) + n * a.ldg : nullptr;
         if (w == 0.f) {
             if (g) {
@@ -551,7 +553,7 @@ __global__ void __launch_bounds__(kRowsThreads, 3) ef_policy_rows_kernel(const P
         const int chunks = chunks_of(sl);
         auto release = [&](int c) {                              // this warp is done with chunk c
             __syncwarp();
-            if (lane == 0) mbar_arrive_relaxed(&s_free[c]);
+            if (lane == 0) mbar_arrive(&s_free[c]);
         };
         Running run = {kLowest, both(0.f)};
         bool ok = true;

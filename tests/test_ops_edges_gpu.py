@@ -54,3 +54,32 @@ def test_policy_loss_passes_on_what_is_not_finite(n, c, with_ref):
             want[t[k]] += coef[k]
             within(out.grad[k], want, 1e-5 * coef[k].abs() + 1e-37, f"grad of row {k}")
     assert bool(out.loss.isnan())
+
+
+def test_policy_loss_of_many_long_rows_passes_on_what_is_not_finite():
+    """The same, by the kernel of many long rows: which rows are NaN, infinite and finite is as with few rows."""
+    n, c = 320, 20000
+    x, t, old, adv, w, ref = policy_case(c, n, c, torch.float32, masked=0.0)
+    for i, (name, value) in enumerate(SPECIAL):
+        {"old": old, "adv": adv, "ref": ref}[name][3 * i] = value
+    many = ops.policy_loss(x, t, old, adv, w, ref_logp=ref, beta=0.1)
+    few = ops.policy_loss(x[:40], t[:40], old[:40], adv[:40], w[:40], ref_logp=ref[:40], beta=0.1)
+    for a, b in ((many.token_loss[:40], few.token_loss), (many.grad[:40], few.grad)):
+        assert torch.equal(a.isnan(), b.isnan()) and torch.equal(a.isinf(), b.isinf())
+    assert bool(many.token_loss[40:].isfinite().all()) and bool(many.grad[40:].isfinite().all()) and bool(many.loss.isnan())
+
+
+@pytest.mark.parametrize("need_grad", [True, False], ids=["gradient", "loss only"])
+def test_many_of_the_longest_rows_repeat_bit_for_bit(need_grad):
+    """Three rows and more per CTA, each loaded over the one before while that is still read: whichever CTA takes a row, and
+    however far its warps are apart, the row's result has the same bits."""
+    n, c = 900, 50257
+    x, t, old, adv, w, ref = policy_case(2, n, c, torch.bfloat16)
+    call = lambda: ops.policy_loss(x, t, old, adv, w, ref_logp=ref, beta=0.04, need_grad=need_grad)  # noqa: E731
+    first = call()
+    e = policy64(x, t, old, adv, w, ref, 0.2, 0.2, 0.04, 1.0)
+    within(first.logp, e["logp"], 1e-5, "logp")
+    for _ in range(6):
+        again = call()
+        assert torch.equal(again.logp, first.logp) and torch.equal(again.token_loss, first.token_loss)
+        assert not need_grad or torch.equal(again.grad, first.grad)
