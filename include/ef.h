@@ -243,9 +243,11 @@ uint32_t* ef_status_word(ef_ctx* ctx);   /* the word itself (device, inside the 
  * ef_debug_build: 1 if this library is the checked build.  ef_debug_shift_tile: test hook of the
  * checked build only (EF_ERR_BAD_STATE otherwise): moves the start of one tile descriptor
  * (tile = -1: the last one) by `delta` elements, between iterations, so that a test can see the
- * check refuse it. */
+ * check refuse it.  ef_debug_wait_limit: test hook of the checked build only, too: attempts after which the device-side
+ * waits of the policy loss give up in the calls that follow (0: at once; negative: as usual). */
 int ef_debug_build(void);
 int ef_debug_shift_tile(ef_ctx* ctx, int64_t tile, int64_t delta);
+int ef_debug_wait_limit(int32_t attempts);
 
 /* Tracing: every entry point that enqueues work runs inside an NVTX range named after itself
  * ("ef_worker_step", "ef_server_step", ...), so that a profiler can group or filter the kernels

@@ -74,6 +74,7 @@ SIGNATURES = {
     "ef_status_word": (_vp, [_vp]),
     "ef_debug_build": (ctypes.c_int, []),
     "ef_debug_shift_tile": (ctypes.c_int, [_vp, _i64, _i64]),
+    "ef_debug_wait_limit": (ctypes.c_int, [_i32]),
     "ef_launch_count": (_i64, [_vp]),
     "ef_worker_step_noalloc": (ctypes.c_int, [_vp, _vp, _vp, _vp, _i64, _f32, _vp, _vp, _vp]),
     "ef_message_units": (_i64, [_vp, _i32, _i32]),
@@ -264,6 +265,11 @@ def ef_debug_build() -> bool:
 
 def ef_debug_shift_tile(ctx: int, tile: int, delta: int) -> None:
     _check(load_library().ef_debug_shift_tile(ctx, tile, delta), "ef_debug_shift_tile")
+
+
+def ef_debug_wait_limit(attempts: int) -> None:
+    """Test hook of the checked build: attempts after which device-side waits of the operators that make a gradient give up."""
+    _check(load_library().ef_debug_wait_limit(attempts), "ef_debug_wait_limit")
 
 
 def ef_status_word(ctx: int) -> Optional[int]:

@@ -5,6 +5,7 @@
 #include "../../include/ef.h"
 #include "ef_kernels.cuh"
 
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 #include <utility>
@@ -138,6 +139,14 @@ inline int cuda_fail(ef_ctx* c, cudaError_t e) {
         cudaError_t e_ = (call);                                 \
         if (e_ != cudaSuccess) return efh::cuda_fail((c), e_);        \
     } while (0)
+
+// Attempts after which the waits of the operators that make a gradient give up; the checked build can set it.
+#ifdef EF_DEBUG
+inline std::atomic<int> g_wait_limit{efk::kMbarWaitLimit};
+inline int wait_limit() { return g_wait_limit.load(std::memory_order_relaxed); }
+#else
+inline constexpr int wait_limit() { return efk::kMbarWaitLimit; }
+#endif
 
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 

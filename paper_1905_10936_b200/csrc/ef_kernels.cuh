@@ -804,8 +804,8 @@ __device__ __forceinline__ bool mbar_try_wait(unsigned long long* bar, unsigned 
                  " selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
     return ok != 0u;
 }
-__device__ __forceinline__ bool mbar_wait_bounded(unsigned long long* bar, unsigned parity) {
-    for (int it = 0; it < kMbarWaitLimit; ++it)
+__device__ __forceinline__ bool mbar_wait_bounded(unsigned long long* bar, unsigned parity, int limit = kMbarWaitLimit) {
+    for (int it = 0; it < limit; ++it)
         if (mbar_try_wait(bar, parity)) return true;
     return false;
 }

@@ -862,6 +862,16 @@ int ef_debug_shift_tile(ef_ctx* c, int64_t tile, int64_t delta) {
 #endif
 }
 
+int ef_debug_wait_limit(int32_t attempts) {
+#ifdef EF_DEBUG
+    efh::g_wait_limit.store(attempts < 0 ? efk::kMbarWaitLimit : attempts, std::memory_order_relaxed);
+    return EF_OK;
+#else
+    (void)attempts;
+    return EF_ERR_BAD_STATE;
+#endif
+}
+
 uint32_t* ef_status_word(ef_ctx* c) { return c ? (uint32_t*)c->status() : nullptr; }
 
 int64_t ef_launch_count(ef_ctx* c) { return c ? c->launches : -1; }

@@ -60,6 +60,7 @@ struct PolicyArgs {
     float lo, hi, beta, inv_t;
     double inv_t64;
     Factor k;
+    int wait_limit;
 };
 
 struct MaxSum { float m, s; };
@@ -230,10 +231,14 @@ __global__ void __launch_bounds__(Shape<GW>::kBlock, Shape<GW>::kCtas) ef_policy
         const int j = tid < sl.head ? tid : sl.tail + (tid - sl.head);
         return j < len && (tid < sl.head || j >= sl.tail) ? j : -1;
     };
+    // A wait that runs out is this thread's last: its group's later rows are NaN, since the parities that it would wait
+    // for no longer say which copy has landed.  (A long row is its CTA's only one, and has a barrier per chunk.)
+    bool ok = true;
+    unsigned in_flight = 0u;                                     // parities of the copies then on their way
     RowHead<T> next;
     auto fetch = [&](long long n, int slot) {
         const Slice<T> sl = slice_of(n);
-        if (tid == 0) {
+        if (tid == 0 && ok) {
             T* const row = reinterpret_cast<T*>(slots + slot * slot_size + sl.phase);
             const int per = per_chunk_of(sl.vecs);
             efk::fence_proxy_async();                            // the slot was last read through ordinary loads
@@ -291,9 +296,12 @@ __global__ void __launch_bounds__(Shape<GW>::kBlock, Shape<GW>::kCtas) ef_policy
                 run.raise(Elem<T>::up(head.edge), k);
                 run.s.x += exp_of(Elem<T>::up(head.edge) - run.m, k);
             }
-            bool ok = true;
             for (int c = 0, at = 0; at < sl.vecs; ++c, at += per) {
-                ok = efk::mbar_wait_bounded(&s_bar[group][slot][c], arrived >> slot & 1u) && ok;
+                if (S::kLong || ok) {
+                    const bool landed = efk::mbar_wait_bounded(&s_bar[group][slot][c], arrived >> slot & 1u, a.wait_limit);
+                    if (!landed && !S::kLong) in_flight = arrived ^ (w_next != 0.f && slice_of(n + step).vecs > 0 ? 0u : 1u << (slot ^ 1));
+                    ok = landed && ok;
+                }
                 const int end = min(sl.vecs, at + per);
                 int i = at + tid;
                 for (; i + kLanes < end; i += 2 * kLanes) {
@@ -313,7 +321,7 @@ __global__ void __launch_bounds__(Shape<GW>::kBlock, Shape<GW>::kCtas) ef_policy
             }
             if (sl.vecs > 0) arrived ^= 1u << slot;
             MaxSum all = {run.m, run.s.x + run.s.y};
-            if (!ok) all.s = nan;                                // a copy did not arrive: the row becomes NaN
+            if (!ok) all.s = nan;
             all = join_warp(all, k);
             if constexpr (GW > 1) {
                 if (lane == 0) s_warp[group][gw] = all;
@@ -388,6 +396,14 @@ __global__ void __launch_bounds__(Shape<GW>::kBlock, Shape<GW>::kCtas) ef_policy
         w = w_next;
         w_next = w_after;
     }
+    if (tid == 0 && !ok) {                                       // copies on their way land before the CTA ends
+        if constexpr (S::kLong) {
+            const int vecs = slice_of((long long)(blockIdx.x / cs)).vecs, per = per_chunk_of(vecs);
+            for (int c = 0, at = 0; at < vecs; ++c, at += per) efk::mbar_wait_bounded(&s_bar[group][0][c], 0u);
+        } else {
+            for (int i = 0; i < 2; ++i) efk::mbar_wait_bounded(&s_bar[group][i][0], in_flight >> i & 1u);
+        }
+    }
 }
 
 // Long rows, many of them: resident CTAs, each of one loading warp and eight that compute.  While a row's gradient is
@@ -435,8 +451,13 @@ __global__ void __launch_bounds__(kRowsThreads, 3) ef_policy_rows_kernel(const P
     __shared__ Row s_row[2];
     __shared__ MaxSum s_warp[GW];
     __shared__ float s_out[3];                                   // maximum, -coef / sum, coef
+    // For a wait that ran out: s_stop ends the CTA's work, the rest says what it leaves.
+    __shared__ unsigned s_stop, s_sent, s_phase;                 // chunks that a copy was sent to, and its phase's parity
+    __shared__ int s_count, s_done, s_asked;                     // rows taken, rows finished, parity of an answer to come or -1
+    __shared__ long long s_taken[4];                             // the rows taken last, by their number
     const int tid = (int)threadIdx.x, lane = tid & 31, gw = tid >> 5, len = a.C;
     if (tid == 0) {
+        s_stop = 0u;
         for (int c = 0; c < kHalves; ++c) { efk::mbar_init(&s_full[c], 1); efk::mbar_init(&s_free[c], GW); }
         for (int b = 0; b < 2; ++b) { efk::mbar_init(&s_known[b], 1); efk::mbar_init(&s_read[b], GW); }
         efk::mbar_init(&s_answered, 1);
@@ -449,22 +470,41 @@ __global__ void __launch_bounds__(kRowsThreads, 3) ef_policy_rows_kernel(const P
     const int per = max(1, ((len / V + kLanes - 1) / kLanes + kHalves - 1) / kHalves) * kLanes;
     auto slice_of = [&](long long n) { return Slice<T>(static_cast<const T*>(a.x) + n * a.ldx, len); };
     auto chunks_of = [&](const Slice<T>& sl) { return (sl.vecs + per - 1) / per; };
+    // The first wait that runs out stops the CTA: it loads and takes no more rows, and no later wait relies on a parity.
+    // (A row that was taken and not finished becomes NaN, see the end.)
+    volatile unsigned* const stop = &s_stop;
+    auto wait = [&](unsigned long long* bar, unsigned parity) {
+        for (int i = 0; i < a.wait_limit; ++i) {
+            if (efk::mbar_try_wait(bar, parity)) return true;
+            if (*stop != 0u) return false;
+        }
+        *stop = 1u;
+        return false;
+    };
 
     if (gw == GW) {                                              // the loading warp
         long long n = blockIdx.x;
-        bool ok = true;
+        bool ok = true, asked = false;
         unsigned freed = 0u;                                     // parity of each chunk's next release
+        unsigned sent = 0u, phase = 0u;                          // chunks filled at least once, parity of the last time
         int used = 0;                                            // chunks that hold a row
-        for (int it = 0;; ++it) {
+        int it = 0;
+        auto all_wait = [&](unsigned long long* bar, unsigned parity) { return __all_sync(kFull, wait(bar, parity)) != 0; };
+        for (;; ++it) {
             Row& row = s_row[it & 1];
             const bool end = n >= a.n;
-            const float w = end ? (ok ? 0.f : -1.f) : a.weight ? __ldg(a.weight + n) : 1.f;
+            if (!end && lane == 0) s_taken[it & 3] = n;
+            const float w = end ? 0.f : a.weight ? __ldg(a.weight + n) : 1.f;
             const Slice<T> sl = slice_of(n);
             const int chunks = chunks_of(sl);
             auto load = [&]() {
                 for (int c = 0; c < max(used, chunks); ++c) {
-                    const bool free = c >= used || efk::mbar_wait_bounded(&s_free[c], freed >> c & 1u);
-                    if (free && c < chunks && lane == 0) {
+                    ok = ok && (c >= used || all_wait(&s_free[c], freed >> c & 1u));
+                    if (!ok) return;
+                    if (c >= chunks) continue;
+                    if (sent >> c & 1u) phase ^= 1u << c;
+                    sent |= 1u << c;
+                    if (lane == 0) {
                         const unsigned bytes = (unsigned)min(per, sl.vecs - c * per) * 16u;
                         efk::fence_proxy_async();                // the chunk was last read through ordinary loads
                         efk::mbar_expect_tx(&s_full[c], bytes);
@@ -487,7 +527,8 @@ __global__ void __launch_bounds__(kRowsThreads, 3) ef_policy_rows_kernel(const P
                 }
                 h.xt = h.t >= 0 && h.t < len ? Elem<T>::up(sl.x[h.t]) : 0.f;
             }
-            if (it >= 2) efk::mbar_wait_bounded(&s_read[it & 1], (it >> 1) + 1 & 1);
+            if (it >= 2) ok = ok && all_wait(&s_read[it & 1], (it >> 1) + 1 & 1);
+            if (!ok) break;
             if (lane == 0) { row.n = end ? -1 : n; row.w = w; row.head = h; }
             if (lane < 2 * V) row.edge[lane] = edge;
             __syncwarp();
@@ -497,141 +538,162 @@ __global__ void __launch_bounds__(kRowsThreads, 3) ef_policy_rows_kernel(const P
                 if (used != 0) load();
                 used = chunks;
             }
+            if (!ok) break;
             if (lane == 0) {
                 efk::fence_proxy_async();                        // the last answer was read through an ordinary load, by this lane
                 ask_for_cta(&s_answer, &s_answered);
             }
-            ok = efk::mbar_wait_bounded(&s_answered, it & 1);
+            asked = true;
+            ok = all_wait(&s_answered, it & 1);
+            if (!ok) break;
+            asked = false;
             int cta = -1;
-            if (ok && lane == 0) cta = taken_cta(&s_answer);
+            if (lane == 0) cta = taken_cta(&s_answer);
             cta = __shfl_sync(kFull, cta, 0);
             n = cta < 0 ? a.n : cta;
         }
-        return;
-    }
-
-    const Factor k = a.k;
-    const float nan = __uint_as_float(0x7fc00000u);
-    unsigned arrived = 0u;                                       // parity of each chunk's next copy
-    long long n = -1;
-    for (int it = 0;; ++it) {
-        const Row& row = s_row[it & 1];
-        if (any_of_warps(!efk::mbar_wait_bounded(&s_known[it & 1], it >> 1 & 1))) break;
-        const float w = row.w;
-        if (row.n < 0) {
-            if (w != 0.f && tid == 0) {                          // a row taken from the grid may be lost: the loss becomes NaN
-                a.logp[n] = nan;
-                if (a.token) a.token[n] = nan;
-            }
-            break;
-        }
-        n = row.n;
-        const RowHead<T> head = row.head;
-        const Slice<T> sl = slice_of(n);
-        const int ends = len - (sl.tail - sl.head);              // logits outside of the vectors
-        const int edge = tid >= ends ? -1 : tid < sl.head ? tid : sl.tail + (tid - sl.head);
-        const T edge_value = row.edge[tid & (2 * V - 1)];
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&s_read[it & 1]);
-        T* const g = a.grad ? static_cast<T*>(a.grad) + n * a.ldg : nullptr;
-        if (w == 0.f) {
-            if (g) {
-                const int first = min(len, (int)((16u - ((uintptr_t)g & 15u)) & 15u) / (int)sizeof(T));
-                const int vecs = (len - first) / V;
-                for (int j = tid; j < first; j += kLanes) g[j] = Elem<T>::down(0.f);
-                for (int i = tid; i < vecs; i += kLanes)
-                    store_once(reinterpret_cast<uint4*>(g + first) + i, make_uint4(0u, 0u, 0u, 0u));
-                for (int j = first + vecs * V + tid; j < len; j += kLanes) g[j] = Elem<T>::down(0.f);
-            }
-            if (tid == 0) {
-                a.logp[n] = 0.f;
-                if (a.token) a.token[n] = 0.f;
-            }
-            continue;
-        }
-        const uint4* const sv = reinterpret_cast<const uint4*>(s_rows);
-        const int chunks = chunks_of(sl);
-        auto release = [&](int c) {                              // this warp is done with chunk c
+        if (lane == 0) { s_count = n >= a.n ? it : it + 1; s_sent = sent; s_phase = phase; s_asked = asked ? it & 1 : -1; }
+    } else {
+        const Factor k = a.k;
+        unsigned arrived = 0u;                                       // parity of each chunk's next copy
+        int it = 0;
+        for (;; ++it) {
+            const Row& row = s_row[it & 1];
+            if (any_of_warps(!wait(&s_known[it & 1], it >> 1 & 1)) || row.n < 0) break;
+            const long long n = row.n;
+            const float w = row.w;
+            const RowHead<T> head = row.head;
+            const Slice<T> sl = slice_of(n);
+            const int ends = len - (sl.tail - sl.head);              // logits outside of the vectors
+            const int edge = tid >= ends ? -1 : tid < sl.head ? tid : sl.tail + (tid - sl.head);
+            const T edge_value = row.edge[tid & (2 * V - 1)];
             __syncwarp();
-            if (lane == 0) mbar_arrive(&s_free[c]);
-        };
-        Running run = {kLowest, both(0.f)};
-        bool ok = true;
-        for (int c = 0; c < chunks; ++c) {
-            ok = efk::mbar_wait_bounded(&s_full[c], arrived >> c & 1u) && ok;
-            const int end = min(sl.vecs, (c + 1) * per);
-            int i = c * per + tid;
-            for (; i + kLanes < end; i += 2 * kLanes) {
-                VecPairs<T> v, u;
-                up_vec<T>(sv[i], v);
-                up_vec<T>(sv[i + kLanes], u);
-                run.raise(fmaxf(run.top_of(v), run.top_of(u)), k);
-                run.add(v, k);
-                run.add(u, k);
+            if (lane == 0) mbar_arrive(&s_read[it & 1]);
+            T* const g = a.grad ? static_cast<T*>(a.grad) + n * a.ldg : nullptr;
+            if (w == 0.f) {
+                if (g) {
+                    const int first = min(len, (int)((16u - ((uintptr_t)g & 15u)) & 15u) / (int)sizeof(T));
+                    const int vecs = (len - first) / V;
+                    for (int j = tid; j < first; j += kLanes) g[j] = Elem<T>::down(0.f);
+                    for (int i = tid; i < vecs; i += kLanes)
+                        store_once(reinterpret_cast<uint4*>(g + first) + i, make_uint4(0u, 0u, 0u, 0u));
+                    for (int j = first + vecs * V + tid; j < len; j += kLanes) g[j] = Elem<T>::down(0.f);
+                }
+                if (tid == 0) {
+                    a.logp[n] = 0.f;
+                    if (a.token) a.token[n] = 0.f;
+                }
+                continue;
             }
-            if (i < end) {
-                VecPairs<T> v;
-                up_vec<T>(sv[i], v);
-                run.raise(run.top_of(v), k);
-                run.add(v, k);
-            }
-            if (!g) release(c);
-        }
-        arrived ^= (1u << chunks) - 1u;
-        if (edge >= 0) {
-            run.raise(Elem<T>::up(edge_value), k);
-            run.s.x += exp_of(Elem<T>::up(edge_value) - run.m, k);
-        }
-        MaxSum all = {run.m, run.s.x + run.s.y};
-        if (!ok) all.s = nan;                                    // a copy did not arrive: the row becomes NaN
-        all = join_warp(all, k);
-        if (lane == 0) s_warp[gw] = all;
-        group_barrier<GW>(0);
-        if (gw == 0) {
-            all = s_warp[lane % GW];
-#pragma unroll
-            for (int o = GW / 2; o > 0; o >>= 1) {
-                MaxSum u;
-                u.m = __shfl_xor_sync(kFull, all.m, o);
-                u.s = __shfl_xor_sync(kFull, all.s, o);
-                all = join(all, u, k);
-            }
-            const Outcome o = outcome_of(a, all, w, head);
-            if (lane == 0) {
-                a.logp[n] = o.logp;
-                if (a.token) a.token[n] = o.token;
-                s_out[0] = all.m; s_out[1] = -o.coef / all.s; s_out[2] = o.coef;
-            }
-        }
-        group_barrier<GW>(0);
-        if (!g) continue;
-        const float m = s_out[0], scale = s_out[1], coef = s_out[2];
-        const int tl = head.t >= 0 && head.t < len ? (int)head.t : -1;
-        auto slope = [&](float v, int j) { return fmaf(exp2_approx((v - m) * k.hi), scale, j == tl ? coef : 0.f); };
-        if ((int)((uintptr_t)g & 15u) == sl.phase) {
-            uint4* const gv = reinterpret_cast<uint4*>(g + sl.head);
+            const uint4* const sv = reinterpret_cast<const uint4*>(s_rows);
+            const int chunks = chunks_of(sl);
+            auto release = [&](int c) {                              // this warp is done with chunk c
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s_free[c]);
+            };
+            Running run = {kLowest, both(0.f)};
+            bool ok = true;
             for (int c = 0; c < chunks; ++c) {
+                ok = ok && wait(&s_full[c], arrived >> c & 1u);
                 const int end = min(sl.vecs, (c + 1) * per);
-#pragma unroll 2
-                for (int i = c * per + tid; i < end; i += kLanes) {
+                int i = c * per + tid;
+                for (; i + kLanes < end; i += 2 * kLanes) {
+                    VecPairs<T> v, u;
+                    up_vec<T>(sv[i], v);
+                    up_vec<T>(sv[i + kLanes], u);
+                    run.raise(fmaxf(run.top_of(v), run.top_of(u)), k);
+                    run.add(v, k);
+                    run.add(u, k);
+                }
+                if (i < end) {
                     VecPairs<T> v;
                     up_vec<T>(sv[i], v);
-#pragma unroll
-                    for (int q = 0; q < V / 2; ++q)
-                        v[q] = mul2(exp2_2(mul2(add2(v[q], both(-m)), both(k.hi))), both(scale));
-                    store_once(gv + i, down_vec<T>(v));
+                    run.raise(run.top_of(v), k);
+                    run.add(v, k);
                 }
-                release(c);
+                if (!g) release(c);
             }
-            // the target's own term, by the thread that wrote its vector
-            if (tl >= sl.head && tl < sl.tail && (tl - sl.head) / V % kLanes == tid)
-                g[tl] = Elem<T>::down(slope(head.xt, tl));
-        } else {                                                 // rows of another phase: element by element
-            const T* const inner = reinterpret_cast<const T*>(sv);
-            for (int j = sl.head + tid; j < sl.tail; j += kLanes) g[j] = Elem<T>::down(slope(Elem<T>::up(inner[j - sl.head]), j));
-            for (int c = 0; c < chunks; ++c) release(c);
+            arrived ^= (1u << chunks) - 1u;
+            if (edge >= 0) {
+                run.raise(Elem<T>::up(edge_value), k);
+                run.s.x += exp_of(Elem<T>::up(edge_value) - run.m, k);
+            }
+            MaxSum all = {run.m, run.s.x + run.s.y};
+            all = join_warp(all, k);
+            if (lane == 0) s_warp[gw] = all;
+            if (any_of_warps(!ok)) break;
+            if (gw == 0) {
+                all = s_warp[lane % GW];
+    #pragma unroll
+                for (int o = GW / 2; o > 0; o >>= 1) {
+                    MaxSum u;
+                    u.m = __shfl_xor_sync(kFull, all.m, o);
+                    u.s = __shfl_xor_sync(kFull, all.s, o);
+                    all = join(all, u, k);
+                }
+                const Outcome o = outcome_of(a, all, w, head);
+                if (lane == 0) {
+                    a.logp[n] = o.logp;
+                    if (a.token) a.token[n] = o.token;
+                    s_out[0] = all.m; s_out[1] = -o.coef / all.s; s_out[2] = o.coef;
+                }
+            }
+            group_barrier<GW>(0);
+            if (!g) continue;
+            const float m = s_out[0], scale = s_out[1], coef = s_out[2];
+            const int tl = head.t >= 0 && head.t < len ? (int)head.t : -1;
+            auto slope = [&](float v, int j) { return fmaf(exp2_approx((v - m) * k.hi), scale, j == tl ? coef : 0.f); };
+            if ((int)((uintptr_t)g & 15u) == sl.phase) {
+                uint4* const gv = reinterpret_cast<uint4*>(g + sl.head);
+                for (int c = 0; c < chunks; ++c) {
+                    const int end = min(sl.vecs, (c + 1) * per);
+    #pragma unroll 2
+                    for (int i = c * per + tid; i < end; i += kLanes) {
+                        VecPairs<T> v;
+                        up_vec<T>(sv[i], v);
+    #pragma unroll
+                        for (int q = 0; q < V / 2; ++q)
+                            v[q] = mul2(exp2_2(mul2(add2(v[q], both(-m)), both(k.hi))), both(scale));
+                        store_once(gv + i, down_vec<T>(v));
+                    }
+                    release(c);
+                }
+                // the target's own term, by the thread that wrote its vector
+                if (tl >= sl.head && tl < sl.tail && (tl - sl.head) / V % kLanes == tid)
+                    g[tl] = Elem<T>::down(slope(head.xt, tl));
+            } else {                                                 // rows of another phase: element by element
+                const T* const inner = reinterpret_cast<const T*>(sv);
+                for (int j = sl.head + tid; j < sl.tail; j += kLanes) g[j] = Elem<T>::down(slope(Elem<T>::up(inner[j - sl.head]), j));
+                for (int c = 0; c < chunks; ++c) release(c);
+            }
+            if (edge >= 0) g[edge] = Elem<T>::down(slope(Elem<T>::up(edge_value), edge));
         }
-        if (edge >= 0) g[edge] = Elem<T>::down(slope(Elem<T>::up(edge_value), edge));
+        if (tid == 0) s_done = it;
+    }
+
+    __syncthreads();
+    if (*stop == 0u) return;
+    // A wait ran out.  The copies and the answer that are on their way land first (waited for as long again); then every row
+    // that this CTA took and did not finish becomes NaN, masked ones too, and with them the loss.
+    if (tid == 0) {
+        for (int c = 0; c < kHalves; ++c) if (s_sent >> c & 1u) efk::mbar_wait_bounded(&s_full[c], s_phase >> c & 1u);
+        if (s_asked >= 0) {
+            const bool answered = efk::mbar_wait_bounded(&s_answered, (unsigned)s_asked);
+            const int cta = answered ? taken_cta(&s_answer) : -1;
+            if (cta >= 0) s_taken[s_count++ & 3] = cta;
+            if (!answered) s_done = min(s_done, s_count - 1);    // a row may be lost
+        }
+    }
+    __syncthreads();
+    const float nan = __uint_as_float(0x7fc00000u);
+    for (int i = s_done; i < s_count; ++i) {
+        const long long n = s_taken[i & 3];
+        if (tid == 0) {
+            a.logp[n] = nan;
+            if (a.token) a.token[n] = nan;
+        }
+        if (a.grad)
+            for (int j = tid; j < len; j += kRowsThreads) static_cast<T*>(a.grad)[n * a.ldg + j] = Elem<T>::down(nan);
     }
 }
 
@@ -744,7 +806,7 @@ int ef_token_logprob(int32_t type, int64_t n, int64_t c, const void* logits, int
     if (n == 0) return EF_OK;
     if (const int rc = efh::check_device()) return rc;
     a.x = logits; a.ldx = ldx; a.target = (const long long*)targets; a.logp = logp;
-    a.n = n; a.C = (int)c;
+    a.n = n; a.C = (int)c; a.wait_limit = efh::wait_limit();
     return launch(type, a, (cudaStream_t)cuda_stream);
 }
 
@@ -773,6 +835,7 @@ int ef_policy_loss(int32_t type, int64_t n, int64_t c, const void* logits, int64
     a.x = logits; a.ldx = ldx; a.target = (const long long*)targets; a.old_logp = old_logp; a.adv = advantages;
     a.weight = weights; a.ref = ref_logp; a.logp = logp; a.token = token_loss; a.grad = grad; a.ldg = ldg;
     a.n = n; a.C = (int)c; a.lo = clip_low; a.hi = clip_high; a.beta = beta;
+    a.wait_limit = efh::wait_limit();
     if (const int rc = launch(type, a, st)) return rc;
     return efh::launch(ef_policy_sum_kernel, 1, kSumThreads, 0, st, 0, (const float*)token_loss, (long long)n, loss);
 }

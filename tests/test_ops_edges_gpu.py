@@ -5,10 +5,24 @@ import math
 import pytest
 import torch
 
+from paper_1905_10936_b200 import binding as ef
+from paper_1905_10936_b200 import build as efbuild
 from paper_1905_10936_b200 import ops
 from test_ops_gpu import policy64, policy_case, within
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture
+def wait_limit():
+    """Sets the attempts after which the operators' waits on the device give up (checked build)."""
+    ef.use_library(efbuild.build_library(debug=True))
+    try:
+        yield ef.ef_debug_wait_limit
+    finally:
+        torch.cuda.synchronize()
+        ef.ef_debug_wait_limit(-1)
+        ef.use_library(None)
 
 
 # ---- policy loss -----------------------------------------------------------------------------
@@ -83,3 +97,31 @@ def test_many_of_the_longest_rows_repeat_bit_for_bit(need_grad):
         again = call()
         assert torch.equal(again.logp, first.logp) and torch.equal(again.token_loss, first.token_loss)
         assert not need_grad or torch.equal(again.grad, first.grad)
+
+
+@pytest.mark.parametrize("n,c,dtype", [(1500, 301, torch.bfloat16), (320, 4000, torch.float32), (9, 50257, torch.float32),
+                                       (3, 300001, torch.bfloat16), (450, 13001, torch.bfloat16), (900, 50257, torch.bfloat16)], ids=str)
+def test_policy_rows_whose_waits_run_out_are_nan(n, c, dtype, wait_limit):
+    """Waits that give up at once, or after a few attempts: the call ends, a row is right or NaN as a whole, the loss is NaN if a
+    row is, and the next call is right again.  Rows of one and four warps, of eight in clusters, many long ones."""
+    x, t, old, adv, w, ref = policy_case(c, n, c, dtype)
+    x[x == -math.inf] = -9.0
+    live = w != 0
+    for need_grad in (True, False):
+        call = lambda: ops.policy_loss(x, t, old, adv, w, ref_logp=ref, beta=0.04, need_grad=need_grad)  # noqa: E731
+        good = call()
+        assert bool(good.token_loss.isfinite().all())
+        for attempts in (0, 1, 3, 20):
+            wait_limit(attempts)
+            for _ in range(3):
+                out = call()
+                lost = out.logp.isnan()
+                assert torch.equal(out.token_loss.isnan(), lost)
+                assert torch.equal(out.logp[~lost], good.logp[~lost]) and torch.equal(out.token_loss[~lost], good.token_loss[~lost])
+                assert bool(out.loss.isnan()) == bool(lost.any())
+                if need_grad:
+                    assert bool(out.grad[lost].isnan().all()) and torch.equal(out.grad[~lost], good.grad[~lost])
+                assert attempts > 0 or bool(lost[live].all())
+        wait_limit(-1)
+        again = call()
+        assert torch.equal(again.logp, good.logp) and torch.equal(again.loss, good.loss)
