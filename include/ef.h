@@ -244,7 +244,7 @@ uint32_t* ef_status_word(ef_ctx* ctx);   /* the word itself (device, inside the 
  * checked build only (EF_ERR_BAD_STATE otherwise): moves the start of one tile descriptor
  * (tile = -1: the last one) by `delta` elements, between iterations, so that a test can see the
  * check refuse it.  ef_debug_wait_limit: test hook of the checked build only, too: attempts after which the device-side
- * waits of the policy loss give up in the calls that follow (0: at once; negative: as usual). */
+ * waits of the policy loss and the weight gradient give up in the calls that follow (0: at once; negative: as usual). */
 int ef_debug_build(void);
 int ef_debug_shift_tile(ef_ctx* ctx, int64_t tile, int64_t delta);
 int ef_debug_wait_limit(int32_t attempts);

@@ -65,7 +65,7 @@ struct WgradArgs {
     int blocks;                                  // stages in all: terms * blocks_n
     int splits;
     float* out; long long ldo;                   // dW, or the partial sums [split][C][J] in the workspace
-    int accumulate;
+    int accumulate, wait_limit;
 };
 
 // ---- tcgen05 -----------------------------------------------------------------------------------
@@ -122,6 +122,12 @@ __device__ __forceinline__ bool elect_one() {
 __device__ __forceinline__ void mbar_arrive(unsigned long long* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(efk::smem_u32(bar)) : "memory");
 }
+// A bounded wait of a whole warp, with the same answer in all lanes: what follows a wait that ran out has barriers in it.
+__device__ __forceinline__ bool wait_warp(unsigned long long* bar, unsigned parity, int limit) {
+    for (int i = 0; i < limit; ++i)
+        if (__all_sync(kFull, efk::mbar_try_wait(bar, parity))) return true;
+    return false;
+}
 // Arrives at the barrier of this offset in the pair's first CTA.
 __device__ __forceinline__ void mbar_arrive_leader(unsigned long long* bar) {
     asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %0, 0;\n"
@@ -160,8 +166,9 @@ template <int N>
 __global__ void __launch_bounds__(kThreadsW, 1) __cluster_dims__(2, 1, 1)
 ef_wgrad_kernel(const WgradArgs a, const __grid_constant__ CUtensorMap codes, const __grid_constant__ CUtensorMap dy) {
     extern __shared__ unsigned char s_raw[];
-    __shared__ unsigned long long s_full[kStages], s_empty[kStages], s_raw_full[kRawStages], s_raw_empty[kRawStages];
-    __shared__ unsigned long long s_acc_full[2], s_acc_empty[2];
+    // full: operand A of the stage (and in the first CTA, both operands of the second's); dy: operand B, by TMA
+    __shared__ unsigned long long s_full[kStages], s_dy[kStages], s_empty[kStages], s_raw_full[kRawStages], s_raw_empty[kRawStages];
+    __shared__ unsigned long long s_acc_full[2], s_acc_empty[2], s_drained;
     __shared__ unsigned s_tmem, s_failed;
     unsigned char* const stage0 = s_raw + ((1024u - (efk::smem_u32(s_raw) & 1023u)) & 1023u);
     unsigned char* const raw0 = stage0 + kStages * kStageBytes<N>;
@@ -175,8 +182,9 @@ ef_wgrad_kernel(const WgradArgs a, const __grid_constant__ CUtensorMap codes, co
     const int total = b1 - b0, spans = (total + kSpan - 1) / kSpan;
     if (tid == kLoadWarp * 32) {
         for (int s = 0; s < kStages; ++s) {
-            // the load warp, the convert warps, and in the first CTA the second's full stage
-            efk::mbar_init(&s_full[s], 1 + kGroupWarps + (rank == 0));
+            // the convert warps, and in the first CTA the second's full stage
+            efk::mbar_init(&s_full[s], kGroupWarps + (rank == 0));
+            efk::mbar_init(&s_dy[s], 1);
             efk::mbar_init(&s_empty[s], 1);
         }
         for (int s = 0; s < kRawStages; ++s) {
@@ -187,6 +195,7 @@ ef_wgrad_kernel(const WgradArgs a, const __grid_constant__ CUtensorMap codes, co
             efk::mbar_init(&s_acc_full[i], 1);
             efk::mbar_init(&s_acc_empty[i], 2 * kConvertWarps);
         }
+        efk::mbar_init(&s_drained, 1);
         efk::mbar_fence_init();
         s_failed = 0u;
     }
@@ -212,7 +221,7 @@ ef_wgrad_kernel(const WgradArgs a, const __grid_constant__ CUtensorMap codes, co
                 acc_at += s_tmem;
                 cluster_wait();
             }
-            ok = ok && efk::mbar_wait_bounded(&s_acc_full[buf], (unsigned)(span >> 1) & 1u);
+            ok = ok && wait_warp(&s_acc_full[buf], (unsigned)(span >> 1) & 1u, a.wait_limit);
             fence_after();
 #pragma unroll
             for (int c = 0; c < kCols; c += 16) tmem_add16(acc_at + (unsigned)(buf * N + c), acc + c);
@@ -247,11 +256,11 @@ ef_wgrad_kernel(const WgradArgs a, const __grid_constant__ CUtensorMap codes, co
             for (int i = 0; i < 6; ++i) {
                 if (t0 + 2 * i >= total) break;
                 const int s = i % 3 * 2, rs = i % 2 * 2;
-                ok = ok && efk::mbar_wait_bounded(&s_raw_full[group + rs], raw_parity ^ (unsigned)(i / 2 & 1));
+                ok = ok && wait_warp(&s_raw_full[group + rs], raw_parity ^ (unsigned)(i / 2 & 1), a.wait_limit);
                 const uint4 q0 = *reinterpret_cast<const uint4*>(from0 + rs * kRawBytes);
                 const uint4 q1 = *reinterpret_cast<const uint4*>(from1 + rs * kRawBytes);
                 const __nv_bfloat162 s2 = __float2bfloat162_rn(__shfl_sync(kFull, sc, (lane & ~3) | turn));
-                ok = ok && efk::mbar_wait_bounded(&s_empty[group + s], i < 3 ? 1u : 0u);
+                ok = ok && wait_warp(&s_empty[group + s], i < 3 ? 1u : 0u, a.wait_limit);
                 if (!ok) break;
                 *reinterpret_cast<uint4*>(to0 + s * kStageBytes<N> + u0) = code_octet(q0.x, q0.y, s2);
                 *reinterpret_cast<uint4*>(to0 + s * kStageBytes<N> + u1) = code_octet(q0.z, q0.w, s2);
@@ -278,10 +287,6 @@ ef_wgrad_kernel(const WgradArgs a, const __grid_constant__ CUtensorMap codes, co
         // result: 32 columns at a time through shared memory, so that a warp stores whole lines.
         // All matrix instructions are done (the last run was collected), so the stages are free.
         asm volatile("bar.sync 1, %0;" ::"n"(kConvertWarps * 32) : "memory");
-        if (s_failed != 0u) {                    // a wait ran out: the tile becomes NaN
-#pragma unroll
-            for (int i = 0; i < kCols; ++i) acc[i] = __uint_as_float(0x7fc00000u);
-        }
         // a warp's 32 x 32 floats, 16-byte units of row r in the order of their number xor (r & 7)
         float4* const buf = reinterpret_cast<float4*>(stage0) + cw * 256;
         const int row0 = i0 + (warp & 3) * 32;
@@ -323,29 +328,45 @@ ef_wgrad_kernel(const WgradArgs a, const __grid_constant__ CUtensorMap codes, co
                 }
             }
         }
+        if (s_failed != 0u) {                    // a wait ran out: what this warp has stored becomes NaN
+            __syncwarp();
+            for (int c = lane; c < kCols; c += 32) {
+                const int j = j0 + (cw >> 2) * kCols + c;
+                for (int r = 0; r < 32; ++r)
+                    if (row0 + r < a.C && j < a.J) out[(long long)(row0 + r) * ldo + j] = __uint_as_float(0x7fc00000u);
+            }
+        }
     } else if (warp == kLoadWarp) {
         const bool one = elect_one();
         int s = 0, rs = 0, block = b0 % a.blocks_n;
         unsigned parity = 1u, raw_parity = 1u;
+        int raw_sent = 0, dy_sent = 0;           // stages under way
         for (int t = 0; t < total; ++t) {
-            if (!efk::mbar_wait_bounded(&s_raw_empty[rs], raw_parity)) { s_failed = 1u; break; }
+            if (!wait_warp(&s_raw_empty[rs], raw_parity, a.wait_limit)) { s_failed = 1u; break; }
+            ++raw_sent;
             if (one) {
                 efk::mbar_expect_tx(&s_raw_full[rs], kRawBytes);
                 tma_load(raw0 + rs * kRawBytes, &codes, i0, block * kTileK, &s_raw_full[rs]);
             }
-            if (!efk::mbar_wait_bounded(&s_empty[s], parity)) { s_failed = 1u; break; }
+            if (!wait_warp(&s_empty[s], parity, a.wait_limit)) { s_failed = 1u; break; }
+            ++dy_sent;
             unsigned char* const dst = stage0 + s * kStageBytes<N> + kTileM * 128;
             if (one) {
-                efk::mbar_expect_tx(&s_full[s], N / 2 * 128);
+                efk::mbar_expect_tx(&s_dy[s], N / 2 * 128);
 #pragma unroll
                 for (int c = 0; c < N / 128; ++c)
-                    tma_load(dst + c * kChunkBytes, &dy, j0 + rank * (N / 2) + 64 * c, (b0 + t) * kTileK, &s_full[s]);
+                    tma_load(dst + c * kChunkBytes, &dy, j0 + rank * (N / 2) + 64 * c, (b0 + t) * kTileK, &s_dy[s]);
             }
             if (++s == kStages) { s = 0; parity ^= 1u; }
             if (++rs == kRawStages) { rs = 0; raw_parity ^= 1u; }
             if (++block == a.blocks_n) block = 0;
         }
         __syncwarp();
+        // No copy is under way when the CTA ends, also where the loop was left early: the last one of each slot lands.
+        for (int i = max(0, raw_sent - kRawStages); i < raw_sent; ++i)
+            wait_warp(&s_raw_full[i % kRawStages], (unsigned)(i / kRawStages) & 1u, efk::kMbarWaitLimit);
+        for (int i = max(0, dy_sent - kStages); i < dy_sent; ++i)
+            wait_warp(&s_dy[i % kStages], (unsigned)(i / kStages) & 1u, efk::kMbarWaitLimit);
         cluster_wait();
         cluster_arrive();
     } else if (rank != 0) {
@@ -356,7 +377,7 @@ ef_wgrad_kernel(const WgradArgs a, const __grid_constant__ CUtensorMap codes, co
         int s = 0;
         unsigned parity = 0u;
         for (int t = 0; t < total; ++t) {
-            if (!efk::mbar_wait_bounded(&s_full[s], parity)) { s_failed = 1u; break; }
+            if (!wait_warp(&s_full[s], parity, a.wait_limit) || !wait_warp(&s_dy[s], parity, a.wait_limit)) { s_failed = 1u; break; }
             if (one) mbar_arrive_leader(&s_full[s]);
             if (++s == kStages) { s = 0; parity ^= 1u; }
         }
@@ -377,8 +398,8 @@ ef_wgrad_kernel(const WgradArgs a, const __grid_constant__ CUtensorMap codes, co
         unsigned parity = 0u;
         unsigned long long da = first;
         for (int t = 0; t < total; ++t) {
-            bool ok = efk::mbar_wait_bounded(&s_full[s], parity);
-            if (at == 0) ok = ok && efk::mbar_wait_bounded(&s_acc_empty[span & 1], ((unsigned)(span >> 1) & 1u) ^ 1u);
+            bool ok = wait_warp(&s_dy[s], parity, a.wait_limit) && wait_warp(&s_full[s], parity, a.wait_limit);
+            if (at == 0) ok = ok && wait_warp(&s_acc_empty[span & 1], ((unsigned)(span >> 1) & 1u) ^ 1u, a.wait_limit);
             if (!ok) { s_failed = 1u; break; }
             fence_after();
             const unsigned d = tmem + (unsigned)((span & 1) * N);
@@ -397,6 +418,9 @@ ef_wgrad_kernel(const WgradArgs a, const __grid_constant__ CUtensorMap codes, co
             if (++s == kStages) { s = 0; parity ^= 1u; da = first; }
         }
         __syncwarp();
+        // Nor is a matrix instruction, which reads both CTAs' stages and writes both CTAs' accumulators.
+        if (one) mma_commit(&s_drained);
+        wait_warp(&s_drained, 0u, efk::kMbarWaitLimit);
         cluster_arrive();
     }
     // No CTA leaves, and none frees its accumulators, while the other may still reach them.
@@ -634,7 +658,7 @@ int ef_checkpoint_weight_grad(int32_t type, int64_t n, int64_t c, int64_t j, con
     a.groups = (int)EF_CHECKPOINT_GROUPS(c);
     a.blocks_n = (int)p.blocks_n; a.blocks = (int)p.blocks; a.splits = p.splits;
     a.out = p.splits > 1 ? (float*)workspace : dw;
-    a.ldo = lddw; a.accumulate = accumulate != 0;
+    a.ldo = lddw; a.accumulate = accumulate != 0; a.wait_limit = efh::wait_limit();
     const int64_t grid = 2 * p.tiles * p.splits;
     if (const int rc = p.tile_n == 256 ? launch_wgrad<256>(a, map_codes, map_dy, grid, st)
                                                  : launch_wgrad<128>(a, map_codes, map_dy, grid, st)) return rc;

@@ -8,7 +8,7 @@ import torch
 from paper_1905_10936_b200 import binding as ef
 from paper_1905_10936_b200 import build as efbuild
 from paper_1905_10936_b200 import ops
-from test_ops_gpu import policy64, policy_case, within
+from test_ops_gpu import policy64, policy_case, randn, within
 
 pytestmark = pytest.mark.gpu
 
@@ -125,3 +125,21 @@ def test_policy_rows_whose_waits_run_out_are_nan(n, c, dtype, wait_limit):
         wait_limit(-1)
         again = call()
         assert torch.equal(again.logp, good.logp) and torch.equal(again.loss, good.loss)
+
+
+# ---- weight gradient -------------------------------------------------------------------------
+@pytest.mark.parametrize("n,c,j,dtype", [(65, 129, 257, torch.bfloat16), (2085, 1001, 777, torch.float32), (8192, 512, 1024, torch.bfloat16),
+                                         (1500, 300, 100, torch.float16)], ids=str)
+def test_weight_gradients_whose_waits_run_out_are_nan(n, c, j, dtype, wait_limit):
+    """Waits that give up at once, or after a few attempts: the call ends, a value is right or NaN, and the next call is right again."""
+    kept, dy = ops.checkpoint_save(randn(n, n, c)), randn(n + 1, n, j, dtype=dtype)
+    good = ops.checkpoint_weight_grad(kept, dy)
+    assert bool(good.isfinite().all())
+    for attempts in (0, 1, 3, 20):
+        wait_limit(attempts)
+        for _ in range(3):
+            out = ops.checkpoint_weight_grad(kept, dy)
+            assert bool(((out == good) | out.isnan()).all())
+            assert attempts > 0 or bool(out.isnan().all())
+    wait_limit(-1)
+    assert torch.equal(ops.checkpoint_weight_grad(kept, dy), good)
