@@ -469,7 +469,9 @@ int ef_worker_step_noalloc(const float* grad, float* momentum, float* residual,
  * Columns are taken in groups of 128.  A group's scale is the smallest power of two s, at least
  * 2^-126, with max|x| <= 127 s (0 for a group of zeros); its codes are x / s rounded to the nearest
  * whole number, ties to even.  It stands for code * s, which is exact in fp32 and bf16.  A group that holds
- * a NaN, an infinity or a magnitude above 127 * 2^121 gets scale NaN and stands for NaN. */
+ * a NaN, an infinity or a magnitude above 127 * 2^121 gets scale NaN and stands for NaN.  In a matrix of type
+ * F16, a value that is finite in fp16 but whose nearest code would stand for 65536 or more gets the code
+ * before it (so 65504 may come back as 64512, and not as an infinity). */
 #define EF_CHECKPOINT_GROUP 128
 #define EF_CHECKPOINT_PITCH(c) (((c) + 15) / 16 * 16)
 #define EF_CHECKPOINT_GROUPS(c) (((c) + EF_CHECKPOINT_GROUP - 1) / EF_CHECKPOINT_GROUP)

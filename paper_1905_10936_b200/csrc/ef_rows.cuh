@@ -24,6 +24,7 @@ template <> struct Elem<float> {
     static __device__ __forceinline__ float down(float v) { return v; }
 };
 template <> struct Elem<__nv_bfloat16> {
+    static constexpr bool kEndsAt65504 = false;
     static __device__ __forceinline__ float up(__nv_bfloat16 v) { return __bfloat162float(v); }
     static __device__ __forceinline__ __nv_bfloat16 down(float v) { return __float2bfloat16_rn(v); }
     static __device__ __forceinline__ float2 up2(unsigned v) {
@@ -35,6 +36,7 @@ template <> struct Elem<__nv_bfloat16> {
     }
 };
 template <> struct Elem<__half> {
+    static constexpr bool kEndsAt65504 = true;
     static __device__ __forceinline__ float up(__half v) { return __half2float(v); }
     static __device__ __forceinline__ __half down(float v) { return __float2half_rn(v); }
     static __device__ __forceinline__ float2 up2(unsigned v) { return __half22float2(*reinterpret_cast<__half2*>(&v)); }
@@ -243,6 +245,8 @@ __device__ __forceinline__ void store8(T* __restrict__ row, int s, int lane, int
 // zeros gets s = 0; one that holds a NaN, an infinity or a value above 127 * 2^121 (within 0.8 %
 // of fp32's largest, where the code's value could overflow) gets s = NaN and decodes to NaN.
 // (1 / s needs neither case: a zero has code 0 by any finite factor, and codes under NaN say nothing.)
+// fp16 ends at 65504, and from scale 1024 on the nearest code of a value just below may stand for 65536, which every fp16 output
+// would turn into an infinity.  So in a matrix of fp16, a value that is finite there gets the last code that is, too.
 constexpr unsigned kLargestCoded = ((127u + 6u + 121u) << 23) | 0x7e0000u;     // bits of 127 * 2^121
 
 struct Scale { float s, inv; };
@@ -293,10 +297,18 @@ __device__ __forceinline__ void encode8(V8& v, int s, int lane, int pitch, int g
         if (lane < 2 && g + lane < groups) scales[g + lane] = lane == 0 ? sc.lo.s : sc.hi.s;
     }
     unsigned f[8];
+    bool near_end = false;
+    if constexpr (sizeof(T) == 2) near_end = Elem<T>::kEndsAt65504 && fmaxf(sc.lo.s, sc.hi.s) >= 1024.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const Scale& q = k < 2 ? sc.lo : sc.hi;
-        const float2 y = fma2(v[k], both(q.inv), both(kMagic));
+        float2 y = fma2(v[k], both(q.inv), both(kMagic));
+        if constexpr (sizeof(T) == 2) {
+            if (near_end) {                      // 65520 is the first value that rounds to an infinity
+                if (fabsf(v[k].x) < 65520.f && fabsf((y.x - kMagic) * q.s) >= 65520.f) y.x -= copysignf(1.f, v[k].x);
+                if (fabsf(v[k].y) < 65520.f && fabsf((y.y - kMagic) * q.s) >= 65520.f) y.y -= copysignf(1.f, v[k].y);
+            }
+        }
         f[2 * k] = __float_as_uint(y.x);
         f[2 * k + 1] = __float_as_uint(y.y);
         v[k] = mul2(add2(y, both(-kMagic)), both(q.s));

@@ -8,7 +8,7 @@ import torch
 from paper_1905_10936_b200 import binding as ef
 from paper_1905_10936_b200 import build as efbuild
 from paper_1905_10936_b200 import ops
-from test_ops_gpu import policy64, policy_case, randn, within
+from test_ops_gpu import F8, policy64, policy_case, quantised, randn, strided, values_of, within
 
 pytestmark = pytest.mark.gpu
 
@@ -143,3 +143,46 @@ def test_weight_gradients_whose_waits_run_out_are_nan(n, c, j, dtype, wait_limit
             assert attempts > 0 or bool(out.isnan().all())
     wait_limit(-1)
     assert torch.equal(ops.checkpoint_weight_grad(kept, dy), good)
+
+
+# ---- checkpoints -----------------------------------------------------------------------------
+def test_fp16_values_stay_finite_in_a_checkpoint():
+    """Every finite fp16 value next to any other: what the checkpoint stands for is finite in fp16, at most one step off where
+    the nearest code would not be and half a step elsewhere, and the operators' fp16 outputs with it."""
+    top = torch.finfo(torch.float16).max
+    x = torch.zeros(4, 256, dtype=torch.float16, device="cuda")
+    x[0] = torch.linspace(-top, top, 256, device="cuda").half()
+    x[1, 0], x[1, 1], x[1, 2], x[1, 3] = top, -top, 65024.0, 64992.0
+    x[1, 130], x[1, 131] = 65024.0, -65024.0                      # a group whose largest has code 127 of scale 512
+    x[2, :128] = -top                                             # a mask
+    x[3, 255] = 65056.0
+    for view in (x, strided(x, 5, 3), x[:, :251]):
+        kept = ops.checkpoint_save(view)
+        back = ops.checkpoint_load(kept, torch.float16)
+        assert bool(back.isfinite().all())
+        assert torch.equal(back.to(F8), values_of(kept))          # no rounding of the values themselves
+        step = kept.scales.to(F8).repeat_interleave(128, dim=1)[:, :view.shape[1]]
+        high = view.to(F8).abs() >= 65024.0
+        off = (values_of(kept) - view.to(F8)).abs()
+        assert bool((off <= torch.where(high, 1.0, 0.5) * step).all())
+        assert torch.equal(values_of(kept)[~high], quantised(view)[~high])
+    assert torch.equal(ops.checkpoint_load(ops.checkpoint_save(x), torch.float16)[1, 130:132], x[1, 130:132])
+    out = ops.activation_forward(x, "gelu", checkpoint_out=True)
+    assert bool(out.a.isfinite().all())
+    out = ops.activation_forward(torch.cat([x, torch.ones_like(x)], dim=1), "swiglu", checkpoint_out=True)
+    assert bool(out.a.isfinite().all())
+    # outputs are computed in fp32: those that round to a finite fp16 value stay finite, others are infinite as they would be without codes
+    h = torch.zeros(2, 200, dtype=torch.float16, device="cuda")
+    h[:, 0] = 1.0
+    w = torch.zeros(200, device="cuda")
+    scale = math.sqrt(200.0)
+    w[0] = 65519.0 / scale * (1 - 1e-6)
+    y = ops.rmsnorm_forward(h, w, 0.0, checkpoint=True).y
+    assert bool(y.isfinite().all()) and float(y[0, 0]) == 64512.0
+    w[0] = 70000.0 / scale
+    plain, kept = ops.rmsnorm_forward(h, w, 0.0), ops.rmsnorm_forward(h, w, 0.0, checkpoint=True)
+    assert plain.y[0, 0] == math.inf and kept.y[0, 0] == math.inf
+    # fp32 and bf16 hold 65536: their checkpoints are as before
+    for dtype in (torch.float32, torch.bfloat16):
+        z = torch.full((1, 8), 65500.0, device="cuda").to(dtype)
+        assert bool((ops.checkpoint_load(ops.checkpoint_save(z), dtype) == 65536.0).all())
