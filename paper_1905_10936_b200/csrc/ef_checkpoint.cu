@@ -148,11 +148,7 @@ struct Forward {
             if constexpr (KIND == EF_ACT_GELU) v[k] = mul2(z[0][k], gelu_gate(z[0][k], mul2(z[0][k], z[0][k])));
             else v[k] = mul2(mul2(z[0][k], sigmoid(z[0][k])), z[P - 1][k]);
         }
-        if (s + kSeg > a.C) {                    // a NaN scale must not reach the padding's codes
-            float* f = reinterpret_cast<float*>(v);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) if (s + Own<T, ALIGNED>::col(lane, k) >= a.C) f[k] = 0.f;
-        }
+        if (s + kSeg > a.C) clear_behind<T, ALIGNED>(v, s, lane, a.C);           // a NaN scale must not reach the padding's codes
         if (a.out_codes)
             encode8<T, ALIGNED>(v, s, lane, a.pitch, a.groups, a.out_codes + before(row, a.pitch), a.out_scales + before(row, a.groups));
         if (a.out) store8<T, ALIGNED>(static_cast<T*>(a.out) + before(row, a.ld_out), s, lane, a.C, v);

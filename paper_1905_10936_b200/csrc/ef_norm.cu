@@ -122,6 +122,8 @@ __global__ void __launch_bounds__(kCtaThreads<W>, kForwardCtas<T, ALIGNED, W, VP
             load_param8<T, ALIGNED>(a.w, s, lane, a.C, w);
 #pragma unroll
             for (int k = 0; k < 4; ++k) h[i][k] = mul2(mul2(h[i][k], both(rstd)), w[k]);
+            if (a.codes && s + kSeg > a.C)       // 0 times a rstd that is not finite must not reach the padding's codes
+                clear_behind<T, ALIGNED>(h[i], s, lane, a.C);
             if (a.codes)
                 encode8<T, ALIGNED>(h[i], s, lane, a.pitch, a.groups, a.codes + before(row, a.pitch),
                                     a.scales + before(row, a.groups));

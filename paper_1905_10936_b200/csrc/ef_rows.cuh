@@ -233,6 +233,14 @@ __device__ __forceinline__ void store8(T* __restrict__ row, int s, int lane, int
     }
 }
 
+// Sets the values of columns >= C to 0.
+template <class T, bool ALIGNED>
+__device__ __forceinline__ void clear_behind(V8& v, int s, int lane, int C) {
+    float* const f = reinterpret_cast<float*>(v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) if (s + Own<T, ALIGNED>::col(lane, k) >= C) f[k] = 0.f;
+}
+
 // ---- the 8-bit checkpoint ----------------------------------------------------------------------
 // A group's scale is the smallest power of two s with max|x| <= 127 s, its codes are
 // rint(x / s) in [-127, 127].  With a power of two, x / s and code * s are exact: the codes do not

@@ -8,7 +8,7 @@ import torch
 from paper_1905_10936_b200 import binding as ef
 from paper_1905_10936_b200 import build as efbuild
 from paper_1905_10936_b200 import ops
-from test_ops_gpu import F8, policy64, policy_case, quantised, randn, strided, values_of, within
+from test_ops_gpu import F8, TYPES, ids, policy64, policy_case, quantised, randn, strided, values_of, within
 
 pytestmark = pytest.mark.gpu
 
@@ -186,3 +186,15 @@ def test_fp16_values_stay_finite_in_a_checkpoint():
     for dtype in (torch.float32, torch.bfloat16):
         z = torch.full((1, 8), 65500.0, device="cuda").to(dtype)
         assert bool((ops.checkpoint_load(ops.checkpoint_save(z), dtype) == 65536.0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("c", [1, 300, 1001, 1004])
+def test_norm_leaves_the_codes_behind_a_row_zero(c, dtype):
+    """Also where rstd is NaN or infinite, which times the nothing behind the row's end is NaN."""
+    x = torch.ones(4, c, dtype=dtype, device="cuda")
+    x[0, c // 2], x[1, c - 1], x[2] = math.nan, math.inf, 0.0
+    out = ops.rmsnorm_forward(x, torch.ones(c, device="cuda"), 0.0, checkpoint=True)
+    assert bool(out.rstd[0].isnan()) and out.rstd[2] == math.inf
+    assert not bool(out.checkpoint.codes[:, c:].any())
+    assert bool(out.y[0].isnan().all()) and bool(out.y[2].isnan().all()) and not bool(out.y[3].isnan().any())
