@@ -110,8 +110,12 @@ __device__ __forceinline__ float2 gelu_gate(float2 z, float2 zz) {
     const float2 t = mul2(z, fma2(zz, both(-kLog2e * kGeluB), both(-kLog2e * kGeluA)));
     return rcp2(add2(both(1.f), exp2_2(t)));
 }
+// z^2 stops at 2^100, where the slope has long been 0 or 1: an infinity would meet the 0 of z s (1 - s).
 __device__ __forceinline__ float2 gelu_slope(float2 z) {
-    const float2 zz = mul2(z, z), s = gelu_gate(z, zz);
+    constexpr float kFar = 1.2676506e30f;
+    float2 zz = mul2(z, z);
+    zz = make_float2(fminf(zz.x, kFar), fminf(zz.y, kFar));
+    const float2 s = gelu_gate(z, zz);
     const float2 rest = fma2(s, both(-1.f), both(1.f));
     return fma2(mul2(mul2(z, s), rest), fma2(zz, both(3.f * kGeluB), both(kGeluA)), s);
 }

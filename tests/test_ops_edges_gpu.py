@@ -198,3 +198,20 @@ def test_norm_leaves_the_codes_behind_a_row_zero(c, dtype):
     assert bool(out.rstd[0].isnan()) and out.rstd[2] == math.inf
     assert not bool(out.checkpoint.codes[:, c:].any())
     assert bool(out.y[0].isnan().all()) and bool(out.y[2].isnan().all()) and not bool(out.y[3].isnan().any())
+
+
+# ---- activation ------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=ids)
+@pytest.mark.parametrize("kind", ["gelu", "swiglu"])
+def test_activation_slope_far_out(kind, dtype):
+    """The slope of a large input is that of the asymptote, as far as a checkpoint's values reach."""
+    big = torch.tensor([1e3, 1e10, 1.7e19, 2e19, 1e25, 1e38, 127 * 2.0 ** 121], device="cuda")
+    c = 128 * len(big)
+    z = torch.zeros(2, c, device="cuda")
+    z[0, ::128], z[1, ::128] = big, -big
+    z = z.to(dtype)
+    if kind == "swiglu":
+        z = torch.cat([z, torch.ones_like(z)], dim=1)
+    out = ops.activation_forward(z, kind)
+    dz = ops.activation_backward(torch.ones(2, c, device="cuda", dtype=dtype), out.z, kind)[:, :c:128]
+    assert bool((dz[0] == 1.0).all()) and bool((dz[1] == 0.0).all())
