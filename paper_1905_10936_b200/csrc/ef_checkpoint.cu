@@ -105,19 +105,34 @@ struct Load {
     }
 };
 
-// sigmoid(2 sqrt(2/pi) (z + 0.044715 z^3)); zz = z * z
-__device__ __forceinline__ float2 gelu_gate(float2 z, float2 zz) {
-    const float2 t = mul2(z, fma2(zz, both(-kLog2e * kGeluB), both(-kLog2e * kGeluA)));
-    return rcp2(add2(both(1.f), exp2_2(t)));
+// s = sigmoid(v) and 1 - s, v = 2 sqrt(2/pi) (z + 0.044715 z^3); zz = z * z.  Exponential and reciprocal are the hardware's
+// approximations.  Outputs of 16 bits round away what they and the difference 1 - s leave (2 to 20 units of 2^-24).  fp32 outputs
+// would show it, 1 - s most of all, which the slope multiplies by up to 20: there the smaller of the two comes from exp(-|v|) <= 1
+// and the larger is the difference (a and dz of 2000 x 1604: 2.3e-8 and 5.0e-8 from 64 bits in the 2-norm, elementary fp32
+// operations 2.5e-8 and 7.3e-8, the short form 3.6e-8 and 1.7e-7).
+struct Gate { float2 s, rest; };
+template <class T>
+__device__ __forceinline__ Gate gelu_gate(float2 z, float2 zz) {
+    if constexpr (sizeof(T) == 4) {
+        const float2 v = mul2(z, fma2(zz, both(kGeluB), both(kGeluA)));
+        const float2 q = exp2_2(mul2(make_float2(fabsf(v.x), fabsf(v.y)), both(-kLog2e)));
+        const float2 small = mul2(q, rcp2(add2(both(1.f), q))), large = fma2(small, both(-1.f), both(1.f));
+        return Gate{make_float2(v.x >= 0.f ? large.x : small.x, v.y >= 0.f ? large.y : small.y),
+                    make_float2(v.x >= 0.f ? small.x : large.x, v.y >= 0.f ? small.y : large.y)};
+    } else {
+        const float2 t = mul2(z, fma2(zz, both(-kLog2e * kGeluB), both(-kLog2e * kGeluA)));
+        const float2 s = rcp2(add2(both(1.f), exp2_2(t)));
+        return Gate{s, fma2(s, both(-1.f), both(1.f))};
+    }
 }
 // z^2 stops at 2^100, where the slope has long been 0 or 1: an infinity would meet the 0 of z s (1 - s).
+template <class T>
 __device__ __forceinline__ float2 gelu_slope(float2 z) {
     constexpr float kFar = 1.2676506e30f;
     float2 zz = mul2(z, z);
     zz = make_float2(fminf(zz.x, kFar), fminf(zz.y, kFar));
-    const float2 s = gelu_gate(z, zz);
-    const float2 rest = fma2(s, both(-1.f), both(1.f));
-    return fma2(mul2(mul2(z, s), rest), fma2(zz, both(3.f * kGeluB), both(kGeluA)), s);
+    const Gate g = gelu_gate<T>(z, zz);
+    return fma2(mul2(mul2(z, g.s), g.rest), fma2(zz, both(3.f * kGeluB), both(kGeluA)), g.s);
 }
 __device__ __forceinline__ float2 sigmoid(float2 g) { return rcp2(add2(both(1.f), exp2_2(mul2(g, both(-kLog2e))))); }
 
@@ -149,7 +164,7 @@ struct Forward {
         V8 v;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            if constexpr (KIND == EF_ACT_GELU) v[k] = mul2(z[0][k], gelu_gate(z[0][k], mul2(z[0][k], z[0][k])));
+            if constexpr (KIND == EF_ACT_GELU) v[k] = mul2(z[0][k], gelu_gate<T>(z[0][k], mul2(z[0][k], z[0][k])).s);
             else v[k] = mul2(mul2(z[0][k], sigmoid(z[0][k])), z[P - 1][k]);
         }
         if (s + kSeg > a.C) clear_behind<T, ALIGNED>(v, s, lane, a.C);           // a NaN scale must not reach the padding's codes
@@ -182,7 +197,7 @@ struct Backward {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if constexpr (KIND == EF_ACT_GELU) {
-                d[0][k] = mul2(da[k], gelu_slope(z[0][k]));
+                d[0][k] = mul2(da[k], gelu_slope<T>(z[0][k]));
             } else {
                 const float2 g = z[0][k], sg = sigmoid(g), das = mul2(da[k], sg);
                 const float2 rest = fma2(sg, both(-1.f), both(1.f));

@@ -8,7 +8,7 @@ import torch
 from paper_1905_10936_b200 import binding as ef
 from paper_1905_10936_b200 import build as efbuild
 from paper_1905_10936_b200 import ops
-from test_ops_gpu import F8, TYPES, ids, policy64, policy_case, quantised, randn, strided, values_of, within
+from test_ops_gpu import F8, TYPES, act64, ids, policy64, policy_case, quantised, randn, slope64, strided, values_of, within
 
 pytestmark = pytest.mark.gpu
 
@@ -215,3 +215,32 @@ def test_activation_slope_far_out(kind, dtype):
     out = ops.activation_forward(z, kind)
     dz = ops.activation_backward(torch.ones(2, c, device="cuda", dtype=dtype), out.z, kind)[:, :c:128]
     assert bool((dz[0] == 1.0).all()) and bool((dz[1] == 0.0).all())
+
+
+@pytest.mark.parametrize("kind", ["gelu", "swiglu"])
+def test_activation_is_as_near_in_fp32_as_elementary_operations(kind):
+    """2-norm distance from 64 bits of a and dz, next to that of the same formulas in elementary fp32 operations, each of
+    which is rounded once.  A quarter more is allowed."""
+    n, c = 64, 4096
+    parts = 2 if kind == "swiglu" else 1
+    z, da = randn(1, n, c * parts, scale=2.0), randn(2, n, c)
+    out = ops.activation_forward(z, kind)
+    got = ops.activation_backward(da, out.z, kind).view(n * parts, c)
+    zq = values_of(out.z)
+    d, _ = slope64(zq, kind)
+    up = da.repeat_interleave(parts, dim=0)
+    want_a, want = act64(zq, kind, c), up.to(F8) * d
+    q = zq.float()
+    if kind == "gelu":
+        v = math.sqrt(2.0 / math.pi) * (q + 0.044715 * q * q * q)
+        th = torch.tanh(v)
+        a = 0.5 * q * (1.0 + th)
+        slope = 0.5 * (1.0 + th) + 0.5 * q * (1.0 - th * th) * math.sqrt(2.0 / math.pi) * (1.0 + 3.0 * 0.044715 * q * q)
+    else:
+        g, u = q[0::2], q[1::2]
+        s = torch.sigmoid(g)
+        a, slope = g * s * u, torch.empty_like(q)
+        slope[0::2], slope[1::2] = u * s * (1.0 + g * (1.0 - s)), g * s
+    for what, mine, plain, exact in (("a", out.a, a, want_a), ("dz", got, up * slope, want)):
+        off, ref = float((mine.to(F8) - exact).norm()), float((plain.to(F8) - exact).norm())
+        assert off <= 1.25 * ref, (what, off, ref)
