@@ -47,7 +47,7 @@ struct ForwardArgs {
     void* h; void* y; float* rstd; signed char* codes; float* scales;
     unsigned n, ldx, ldr, ldh, ldy;
     int C, pitch, groups;
-    float eps, inv_c;
+    double eps, inv_c;                   // the last step of rstd in 64 bits: one rounding after the sum's own
 };
 
 // Both passes walk over rows with all CTAs of the grid resident, and load the next row's values, in
@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(kCtaThreads<W>, kForwardCtas<T, ALIGNED, W, VP
         }
         const float ss = row_sum<W>(ss2.x + ss2.y, s_part[group], parity, group, warp, lane);
         parity ^= 1;
-        const float rstd = 1.f / sqrtf(fmaf(ss, a.inv_c, a.eps));
+        const float rstd = (float)rsqrt(fma((double)ss, a.inv_c, a.eps));
         if (warp == 0 && lane == 0) a.rstd[row] = rstd;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
@@ -343,7 +343,7 @@ int ef_rmsnorm_forward(int32_t type, int64_t n, int64_t c, const void* x, int64_
     a.x = x; a.r = r; a.w = w; a.h = h; a.y = y; a.rstd = rstd; a.codes = (signed char*)codes; a.scales = scales;
     a.n = (unsigned)n; a.ldx = (unsigned)ldx; a.ldr = (unsigned)ldr; a.ldh = (unsigned)ldh; a.ldy = (unsigned)ldy;
     a.C = (int)c; a.pitch = (int)EF_CHECKPOINT_PITCH(c); a.groups = (int)EF_CHECKPOINT_GROUPS(c);
-    a.eps = eps; a.inv_c = 1.f / (float)c;
+    a.eps = (double)eps; a.inv_c = 1.0 / (double)c;
     return efh::with_type(type, [&](auto t) {
         using T = decltype(t);
         return with_shape<T, false>(c, [&](auto w_, auto v_) {

@@ -8,7 +8,7 @@ import torch
 from paper_1905_10936_b200 import binding as ef
 from paper_1905_10936_b200 import build as efbuild
 from paper_1905_10936_b200 import ops
-from test_ops_gpu import F8, TYPES, act64, ids, policy64, policy_case, quantised, randn, slope64, strided, values_of, within
+from test_ops_gpu import EPS, F8, TYPES, act64, gen, ids, policy64, policy_case, quantised, randn, slope64, strided, values_of, within
 
 pytestmark = pytest.mark.gpu
 
@@ -244,3 +244,15 @@ def test_activation_is_as_near_in_fp32_as_elementary_operations(kind):
     for what, mine, plain, exact in (("a", out.a, a, want_a), ("dz", got, up * slope, want)):
         off, ref = float((mine.to(F8) - exact).norm()), float((plain.to(F8) - exact).norm())
         assert off <= 1.25 * ref, (what, off, ref)
+
+
+# ---- norm ------------------------------------------------------------------------------------
+@pytest.mark.parametrize("c", [7, 1000, 1603, 4096])
+def test_norm_rstd_is_rounded_once(c):
+    """Whole numbers whose squares add up to less than 2^24: the sum is exact, so rstd is the rounded 64-bit value."""
+    n = 500
+    x = torch.randint(-40, 41, (n, c), device="cuda", generator=gen(c)).float()
+    x[torch.arange(n, device="cuda"), torch.arange(n, device="cuda") % c] = 2000.0
+    want = 1.0 / torch.sqrt((x.to(F8) ** 2).mean(dim=1) + float(torch.tensor(EPS)))
+    assert float((x.to(F8) ** 2).sum(dim=1).max()) < 2.0 ** 24
+    assert torch.equal(ops.rmsnorm_forward(x, torch.ones(c, device="cuda"), EPS).rstd, want.float())
