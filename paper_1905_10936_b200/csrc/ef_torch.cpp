@@ -4,6 +4,7 @@
 // library is the one that the binding has loaded: its functions come in through bind().
 #include <Python.h>
 
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_strided.h>
 #include <c10/cuda/CUDAGuard.h>
@@ -127,6 +128,11 @@ at::Tensor fresh_checkpoint(int64_t n, int64_t c, c10::Device device) {
 int8_t* codes_of(const at::Tensor& t) { return t.defined() ? (int8_t*)t.data_ptr() : nullptr; }
 float* scales_of(const at::Tensor& t, int64_t n, int64_t c) {
     return t.defined() ? (float*)((char*)t.data_ptr() + n * EF_CHECKPOINT_PITCH(c)) : nullptr;
+}
+// As torch does, a leaf that requires gradients, or a view of one, is not overwritten while gradients are recorded.
+void check_overwritable(const at::Tensor& t, const char* name) {
+    if (at::GradMode::is_enabled() && t.requires_grad() && (t.is_leaf() || (t.is_view() && t._base().is_leaf())))
+        refuse(std::string(name) + ": a leaf that requires gradients would be overwritten");
 }
 // The library wrote to a tensor of the caller's: a backward pass that has saved its old values must notice.
 void written(const at::Tensor& t) {
@@ -256,6 +262,7 @@ PyObject* checkpoint_weight_grad(PyObject* const* a) {   // checkpoint of x (5),
     const Matrix dy = matrix(a[5], "dy");
     const at::Tensor* const given = optional_tensor(a[6], "out");
     const bool accumulate = truth(a[7]);
+    if (given) check_overwritable(*given, "out");
     const c10::Device device = dy.t.device();
     if (k.rows != dy.n || k.device != device.index()) refuse("x: a checkpoint of dy's rows is needed");
     if (!given && accumulate) refuse("accumulate: needs out");
@@ -300,6 +307,7 @@ PyObject* policy_loss(PyObject* const* a) {
     const float lo = (float)number(a[6]), hi = (float)number(a[7]), beta = (float)number(a[8]), temperature = (float)number(a[9]);
     const bool need_grad = truth(a[10]), in_place = truth(a[11]);
     const c10::Device device = x.t.device();
+    if (need_grad && in_place) check_overwritable(x.t, "logits");
     at::Tensor grad;
     if (need_grad) grad = in_place ? x.t : fresh({x.n, x.c}, x.t.scalar_type(), device);
     at::Tensor loss = fresh({}, at::kFloat, device), logp = fresh({x.n}, at::kFloat, device), token = fresh({x.n}, at::kFloat, device);

@@ -6,6 +6,12 @@ Matrices are 2-D CUDA tensors with neighbouring columns (``stride(1) == 1``; row
 or start anywhere) of type float32, bfloat16 or float16.  Work is enqueued on the device's current
 stream; a tensor made on another stream has to be complete there first (``Stream.wait_stream``),
 and ``Tensor.record_stream`` is the caller's, as for any torch operator.
+
+The functions are the two halves of a pass, forward and backward, and not differentiable calls: torch
+records no graph through them, whether their inputs require gradients or not.  A forward function's
+results go to its backward function, and gradients where the caller wants them (``policy_loss(...).grad``
+into ``logits.backward(grad)``, for instance).  ``in_place`` and ``out`` refuse a leaf that requires
+gradients while gradients are recorded, as torch's own in-place operators do.
 """
 from __future__ import annotations
 

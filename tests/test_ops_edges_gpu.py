@@ -256,3 +256,29 @@ def test_norm_rstd_is_rounded_once(c):
     want = 1.0 / torch.sqrt((x.to(F8) ** 2).mean(dim=1) + float(torch.tensor(EPS)))
     assert float((x.to(F8) ** 2).sum(dim=1).max()) < 2.0 ** 24
     assert torch.equal(ops.rmsnorm_forward(x, torch.ones(c, device="cuda"), EPS).rstd, want.float())
+
+
+# ---- tensors that torch differentiates -------------------------------------------------------
+def test_leaves_that_require_gradients_are_not_overwritten():
+    x, t, old, adv, w, _ = policy_case(1, 5, 40, torch.float32)
+    leaf = x.clone().requires_grad_()
+    for bad in (leaf, leaf[1:4]):
+        k = bad.shape[0]
+        with pytest.raises(ValueError, match="requires gradients"):
+            ops.policy_loss(bad, t[:k], old[:k], adv[:k], w[:k], in_place=True)
+    assert torch.equal(leaf.detach(), x)
+    ops.policy_loss(leaf, t, old, adv, w)                         # read only
+    ops.policy_loss(leaf, t, old, adv, w, need_grad=False, in_place=True)
+    kept, dy = ops.checkpoint_save(x.nan_to_num(neginf=0.0)), torch.ones(5, 8, device="cuda")
+    weight = torch.zeros(40, 8, device="cuda", requires_grad=True)
+    with pytest.raises(ValueError, match="requires gradients"):
+        ops.checkpoint_weight_grad(kept, dy, out=weight)
+    assert not bool(weight.detach().any())
+    with torch.no_grad():
+        ops.checkpoint_weight_grad(kept, dy, out=weight)
+        ops.policy_loss(leaf, t, old, adv, w, in_place=True)
+    base = torch.zeros(3, 40, requires_grad=True, device="cuda")  # logits of a model, whose backward pass does not need them
+    logits = base * 2.0 + x[:3].nan_to_num(neginf=-9.0)
+    out = ops.policy_loss(logits, t[:3], old[:3], adv[:3], w[:3], in_place=True)
+    logits.backward(out.grad)
+    assert torch.equal(base.grad, 2.0 * out.grad)
