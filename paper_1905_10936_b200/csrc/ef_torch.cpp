@@ -106,7 +106,8 @@ bool truth(PyObject* o) {
     if (v < 0) throw Refused{};
     return v != 0;
 }
-// A checkpoint as ops.Checkpoint describes it: rows, columns, device, addresses of codes and scales.
+// A checkpoint as ops.Checkpoint describes it: rows, columns, and its codes and scales, or one buffer with both and None.
+// The addresses are those of the tensors at this call: they may have been copied or unpickled since.
 struct Kept {
     int64_t rows, cols;
     int device;
@@ -114,7 +115,18 @@ struct Kept {
     float* scales;
 };
 Kept kept(PyObject* const* a) {
-    return Kept{integer(a[0]), integer(a[1]), (int)integer(a[2]), (int8_t*)integer(a[3]), (float*)integer(a[4])};
+    const int64_t n = integer(a[0]), c = integer(a[1]);
+    const at::Tensor& first = tensor(a[2], "checkpoint");
+    const at::Tensor* const scales = optional_tensor(a[3], "checkpoint");
+    auto holds = [](const at::Tensor& t, at::ScalarType type, int64_t count) {
+        return t.is_cuda() && t.scalar_type() == type && t.is_contiguous() && t.numel() == count;
+    };
+    const int64_t codes = n * EF_CHECKPOINT_PITCH(c), groups = n * EF_CHECKPOINT_GROUPS(c);
+    if (n < 0 || c < 1 || !holds(first, at::kChar, scales ? codes : codes + 4 * groups) ||
+        (scales && (!holds(*scales, at::kFloat, groups) || scales->device() != first.device())))
+        refuse("checkpoint: its codes and scales are not on a CUDA device, or not of its size");
+    int8_t* const p = (int8_t*)first.data_ptr();
+    return Kept{n, c, (int)first.get_device(), p, scales ? (float*)scales->data_ptr() : (float*)(p + codes)};
 }
 
 // ---- results -----------------------------------------------------------------------------------
@@ -172,7 +184,7 @@ PyObject* checkpoint_save(PyObject* const* a) {
 
 PyObject* checkpoint_load(PyObject* const* a) {
     const Kept k = kept(a);
-    const int type = (int)integer(a[5]);
+    const int type = (int)integer(a[4]);
     const c10::Device device(c10::kCUDA, (c10::DeviceIndex)k.device);
     at::Tensor x = fresh({k.rows, k.cols}, type == EF_TYPE_F32 ? at::kFloat : type == EF_TYPE_BF16 ? at::kBFloat16 : at::kHalf, device);
     const On on(device);
@@ -201,12 +213,12 @@ PyObject* rmsnorm_forward(PyObject* const* a) {          // x, weight, eps, resi
     return pack(std::move(h), std::move(y), std::move(rstd), std::move(b));
 }
 
-PyObject* rmsnorm_backward(PyObject* const* a) {         // dy, h or None, its checkpoint (5), weight, rstd, dh -> dx, dw
+PyObject* rmsnorm_backward(PyObject* const* a) {         // dy, h or None, its checkpoint (4), weight, rstd, dh -> dx, dw
     const Matrix dy = matrix(a[0], "dy");
     const at::Tensor* const ht = optional_tensor(a[1], "h");
-    const float* const w = (const float*)vec(a[7], dy.c, "weight", dy);
-    const float* const rstd = (const float*)vec(a[8], dy.n, "rstd", dy);
-    const at::Tensor* const dht = optional_tensor(a[9], "dh");
+    const float* const w = (const float*)vec(a[6], dy.c, "weight", dy);
+    const float* const rstd = (const float*)vec(a[7], dy.n, "rstd", dy);
+    const at::Tensor* const dht = optional_tensor(a[8], "dh");
     const c10::Device device = dy.t.device();
     std::optional<Matrix> h, dh;
     Kept k = {};
@@ -243,7 +255,7 @@ PyObject* activation_forward(PyObject* const* a) {       // z, kind, checkpoint,
     return pack(std::move(out), std::move(bz), std::move(ba));
 }
 
-PyObject* activation_backward(PyObject* const* a) {      // da, kind, checkpoint of z (5) -> dz
+PyObject* activation_backward(PyObject* const* a) {      // da, kind, checkpoint of z (4) -> dz
     const Matrix da = matrix(a[0], "da");
     const int kind = (int)integer(a[1]), parts = kind == EF_ACT_SWIGLU ? 2 : 1;
     const Kept k = kept(a + 2);
@@ -257,11 +269,11 @@ PyObject* activation_backward(PyObject* const* a) {      // da, kind, checkpoint
     return wrapped(std::move(dz));
 }
 
-PyObject* checkpoint_weight_grad(PyObject* const* a) {   // checkpoint of x (5), dy, out or None, accumulate -> out
+PyObject* checkpoint_weight_grad(PyObject* const* a) {   // checkpoint of x (4), dy, out or None, accumulate -> out
     const Kept k = kept(a);
-    const Matrix dy = matrix(a[5], "dy");
-    const at::Tensor* const given = optional_tensor(a[6], "out");
-    const bool accumulate = truth(a[7]);
+    const Matrix dy = matrix(a[4], "dy");
+    const at::Tensor* const given = optional_tensor(a[5], "out");
+    const bool accumulate = truth(a[6]);
     if (given) check_overwritable(*given, "out");
     const c10::Device device = dy.t.device();
     if (k.rows != dy.n || k.device != device.index()) refuse("x: a checkpoint of dy's rows is needed");
@@ -280,8 +292,8 @@ PyObject* checkpoint_weight_grad(PyObject* const* a) {   // checkpoint of x (5),
                                      accumulate, bytes ? work.data_ptr() : nullptr, bytes, on.stream), "ef_checkpoint_weight_grad");
     if (given) {
         written(out);
-        Py_INCREF(a[6]);
-        return a[6];
+        Py_INCREF(a[5]);
+        return a[5];
     }
     return wrapped(std::move(out));
 }
@@ -356,8 +368,8 @@ PyObject* entry(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define EF_ENTRY(f, n) {#f, (PyCFunction)(void (*)(void))entry<f, n>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, nullptr},
-    EF_ENTRY(checkpoint_save, 1), EF_ENTRY(checkpoint_load, 6), EF_ENTRY(rmsnorm_forward, 5), EF_ENTRY(rmsnorm_backward, 10),
-    EF_ENTRY(activation_forward, 4), EF_ENTRY(activation_backward, 7), EF_ENTRY(checkpoint_weight_grad, 8),
+    EF_ENTRY(checkpoint_save, 1), EF_ENTRY(checkpoint_load, 5), EF_ENTRY(rmsnorm_forward, 5), EF_ENTRY(rmsnorm_backward, 9),
+    EF_ENTRY(activation_forward, 4), EF_ENTRY(activation_backward, 6), EF_ENTRY(checkpoint_weight_grad, 7),
     EF_ENTRY(token_logprob, 3), EF_ENTRY(policy_loss, 12), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ef_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

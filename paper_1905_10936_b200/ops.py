@@ -60,7 +60,7 @@ class Checkpoint:
     """An n x cols matrix kept in 8 bits: codes [n, pitch] int8 and scales [n, groups] float32,
     both contiguous (layout as in include/ef.h)."""
 
-    __slots__ = ("rows", "cols", "_buffer", "_codes", "_scales", "_where")
+    __slots__ = ("rows", "cols", "_where")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int):
         n = codes.shape[0]
@@ -69,43 +69,40 @@ class Checkpoint:
                 and scales.is_contiguous() and scales.shape == (n, checkpoint_groups(cols))
                 and scales.get_device() == codes.get_device()):
             raise ValueError("codes and scales do not make a checkpoint of this width")
-        self.rows, self.cols, self._buffer, self._codes, self._scales = n, cols, None, codes, scales
-        self._where = (n, cols, codes.get_device(), codes.data_ptr(), scales.data_ptr())
+        self.rows, self.cols = n, cols
+        self._where = (n, cols, codes, scales)
 
     @classmethod
     def _of(cls, buffer: torch.Tensor, n: int, cols: int) -> "Checkpoint":
         """The checkpoint in one buffer, codes first, as the native half allocates it."""
         self = object.__new__(cls)
-        at = buffer.data_ptr()
-        self.rows, self.cols, self._buffer, self._codes, self._scales = n, cols, buffer, None, None
-        self._where = (n, cols, buffer.get_device(), at, at + n * checkpoint_pitch(cols))
+        self.rows, self.cols = n, cols
+        self._where = (n, cols, buffer, None)
         return self
 
     @property
     def codes(self) -> torch.Tensor:
-        if self._codes is None:
-            pitch = checkpoint_pitch(self.cols)
-            self._codes = self._buffer[:self.rows * pitch].view(self.rows, pitch)
-        return self._codes
+        n, cols, first, scales = self._where
+        return first if scales is not None else first[:n * checkpoint_pitch(cols)].view(n, checkpoint_pitch(cols))
 
     @property
     def scales(self) -> torch.Tensor:
-        if self._scales is None:
-            at = self.rows * checkpoint_pitch(self.cols)
-            self._scales = self._buffer[at:].view(torch.float32).view(self.rows, checkpoint_groups(self.cols))
-        return self._scales
+        n, cols, first, scales = self._where
+        if scales is not None:
+            return scales
+        return first[n * checkpoint_pitch(cols):].view(torch.float32).view(n, checkpoint_groups(cols))
 
     def nbytes(self) -> int:
         return self.rows * (checkpoint_pitch(self.cols) + 4 * checkpoint_groups(self.cols))
 
     def record_stream(self, stream: torch.cuda.Stream) -> None:
         """Marks the memory as used on another stream, as Tensor.record_stream."""
-        for t in (self._buffer, self._codes, self._scales):
+        for t in self._where[2:]:
             if t is not None:
                 t.record_stream(stream)
 
 
-_NONE = (0, 0, 0, 0, 0)                  # no checkpoint
+_NONE = (0, 0, None, None)               # no checkpoint
 
 
 def checkpoint_save(x: torch.Tensor) -> Checkpoint:

@@ -1,0 +1,41 @@
+"""Edges of the operators that make a worker's gradient that need no GPU."""
+import copy
+import pickle
+
+import pytest
+import torch
+
+from paper_1905_10936_b200 import binding as ef
+from paper_1905_10936_b200 import build as efbuild
+from paper_1905_10936_b200 import ops
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    efbuild.build_library()
+    efbuild.build_torch_binding()
+
+
+def host_checkpoint(n, c):
+    """A checkpoint whose memory is on the host: no call takes it."""
+    size = n * ops.checkpoint_pitch(c) + 4 * n * ops.checkpoint_groups(c)
+    return ops.Checkpoint._of(torch.randint(-127, 128, (size,), dtype=torch.int8), n, c)
+
+
+@pytest.mark.parametrize("how", [copy.deepcopy, lambda k: pickle.loads(pickle.dumps(k))], ids=["deepcopy", "pickle"])
+def test_a_copied_checkpoint_refers_to_its_own_memory(how):
+    kept = host_checkpoint(3, 200)
+    other = how(kept)
+    assert (other.rows, other.cols) == (3, 200) and torch.equal(other.codes, kept.codes)
+    assert not any(isinstance(v, int) and v > 1 << 20 for v in other._where), "an address"
+    before = kept.codes.clone()
+    other.codes.zero_()
+    assert torch.equal(kept.codes, before) and not bool(other._where[2][:other.codes.numel()].any())
+
+
+def test_a_checkpoint_that_is_not_on_a_gpu_is_refused():
+    """As one that was unpickled to the host is: its addresses mean nothing there."""
+    kept = host_checkpoint(4, 40)
+    for call in (lambda: ops.checkpoint_load(kept), lambda: ops.checkpoint_weight_grad(kept, torch.ones(4, 8))):
+        with pytest.raises(ValueError, match="CUDA"):
+            call()

@@ -1,6 +1,8 @@
 """Values at which the operators that make a worker's gradient could go wrong: NaN and infinities where they must come
 through, the ends of a type's range, padding, row shapes between the usual ones, and bounds that hold their precision."""
+import copy
 import math
+import pickle
 
 import pytest
 import torch
@@ -186,6 +188,20 @@ def test_fp16_values_stay_finite_in_a_checkpoint():
     for dtype in (torch.float32, torch.bfloat16):
         z = torch.full((1, 8), 65500.0, device="cuda").to(dtype)
         assert bool((ops.checkpoint_load(ops.checkpoint_save(z), dtype) == 65536.0).all())
+
+
+@pytest.mark.parametrize("own", [False, True], ids=["one buffer", "two tensors"])
+def test_copies_of_a_checkpoint_outlive_it(own):
+    x = randn(1, 70, 300)
+    kept = ops.checkpoint_save(x)
+    if own:
+        kept = ops.Checkpoint(kept.codes.clone(), kept.scales.clone(), 300)
+    want, grad = ops.checkpoint_load(kept), ops.checkpoint_weight_grad(kept, x)
+    others = [copy.deepcopy(kept), pickle.loads(pickle.dumps(kept))]
+    kept.codes.fill_(77)
+    kept.scales.fill_(1.0)
+    for other in others:
+        assert torch.equal(ops.checkpoint_load(other), want) and torch.equal(ops.checkpoint_weight_grad(other, x), grad)
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=ids)
