@@ -454,8 +454,9 @@ int ef_worker_step_noalloc(const float* grad, float* momentum, float* residual,
  *   - an output may be one of the call's inputs (same pointer, stride and type) where the call says
  *     so; otherwise buffers must not overlap.
  *   - work is enqueued on cuda_stream without synchronisation, and nothing is allocated.
- *   - errors: INVALID_ARG (a size, stride, type or missing pointer), TOO_LARGE (2^31 rows or a stride of 2^31
- *     elements and more, or a width past the call's limit), WORKSPACE, ALIGNMENT (a pointer that is
+ *   - errors: INVALID_ARG (a size, stride, type or missing pointer), TOO_LARGE (a width past the call's limit; 2^31
+ *     rows and more, but for short rows of the policy loss; a stride of 2^31 elements and more, but for the policy
+ *     loss and the weight gradient), WORKSPACE, ALIGNMENT (a pointer that is
  *     not aligned to its element, or codes not to 16 bytes), UNSUPPORTED_DEVICE, CUDA.
  *   - kernels are launched with programmatic stream serialization, wait on the device for the kernel before them on
  *     the stream, and do not signal early. */

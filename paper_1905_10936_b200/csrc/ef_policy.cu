@@ -786,7 +786,7 @@ bool set_temperature(PolicyArgs& a, float temperature) {
 
 int check_logits(int32_t type, int64_t n, int64_t c, const void* x, int64_t ldx, const int64_t* target, const float* logp) {
     if (!efh::type_ok(type) || n < 0 || c < 1 || ldx < c) return EF_ERR_INVALID_ARG;
-    if (c * (int64_t)efh::type_size(type) > (int64_t)kMaxCluster * kMaxSliceBytes) return EF_ERR_TOO_LARGE;
+    if (c > (int64_t)kMaxCluster * kMaxSliceBytes / (int64_t)efh::type_size(type)) return EF_ERR_TOO_LARGE;
     if (n == 0) return EF_OK;
     if (!x || !target || !logp) return EF_ERR_INVALID_ARG;
     if (!efh::natural(Mat{x, ldx, type}) || ((uintptr_t)target & 7u) || ((uintptr_t)logp & 3u)) return EF_ERR_ALIGNMENT;

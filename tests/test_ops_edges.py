@@ -39,3 +39,15 @@ def test_a_checkpoint_that_is_not_on_a_gpu_is_refused():
     for call in (lambda: ops.checkpoint_load(kept), lambda: ops.checkpoint_weight_grad(kept, torch.ones(4, 8))):
         with pytest.raises(ValueError, match="CUDA"):
             call()
+
+
+BUF = 4096                                   # any non-null, aligned value: never dereferenced on the host
+
+
+def test_widths_whose_bytes_overflow_are_too_large():
+    for dtype, c in ((0, (1 << 62) + 8), (1, (1 << 63) - 8), (0, 409601), (1, 819201)):
+        for name, args in (("ef_token_logprob", (dtype, 4, c, BUF, c, BUF, 1.0, BUF, 0)),
+                           ("ef_policy_loss", (dtype, 4, c, BUF, c, BUF, BUF, BUF, BUF, None, 0.2, 0.2, 0.0, 1.0, BUF, BUF, BUF, None, 0, 0))):
+            with pytest.raises(ef.EFError) as ei:
+                getattr(ef, name)(*args)
+            assert ei.value.status == ef.EF_ERR_TOO_LARGE, (name, c)
