@@ -547,7 +547,7 @@ Plan plan_of(int32_t type, int64_t n, int64_t c, int64_t j, bool direct) {
 }
 
 bool reads_direct(int32_t type, const void* dy, int64_t ldy) {
-    return type == EF_TYPE_BF16 && efh::aligned16(dy) && ldy % 8 == 0;
+    return type == EF_TYPE_BF16 && efh::aligned16(dy) && ldy % 8 == 0 && ldy < (int64_t)1 << 39;      // TMA strides: below 2^40 bytes
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,

@@ -51,3 +51,9 @@ def test_widths_whose_bytes_overflow_are_too_large():
             with pytest.raises(ef.EFError) as ei:
                 getattr(ef, name)(*args)
             assert ei.value.status == ef.EF_ERR_TOO_LARGE, (name, c)
+
+
+def test_a_stride_past_the_copy_engine_s_limit_goes_through_the_workspace():
+    need = ef.ef_checkpoint_weight_grad_workspace_bytes
+    assert need(1, 1, 128, 128, BUF, (1 << 39) - 8) == 0
+    assert need(1, 1, 128, 128, BUF, 1 << 39) >= 64 * 128 * 2
