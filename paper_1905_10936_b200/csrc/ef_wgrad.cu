@@ -506,13 +506,7 @@ struct Plan {
 };
 
 constexpr int kPairs = efh::kSMs / 2;
-#ifndef K128
-#define K128 420
-#define K256 500
-#define T128 4200
-#define T256 5800
-#endif
-constexpr double kStageNs[2] = {K128, K256}, kTileNs[2] = {T128, T256};      // of 256 x 128 and 256 x 256
+constexpr double kStageNs[2] = {420, 500}, kTileNs[2] = {4200, 5800};          // of 256 x 128 and 256 x 256
 
 Plan plan_of(int32_t type, int64_t n, int64_t c, int64_t j, bool direct) {
     Plan p;
