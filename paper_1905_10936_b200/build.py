@@ -54,16 +54,20 @@ def build_library(force: bool = False, verbose: bool = False, debug: bool = Fals
 
 
 def build_torch_binding(force: bool = False) -> str:
-    """Builds _ef_torch.so in-tree with g++ against the installed torch."""
-    if not force and os.path.exists(TORCH_BINDING):
-        if os.path.getmtime(TORCH_BINDING) >= max(os.path.getmtime(p) for p in TORCH_SOURCES):
-            return TORCH_BINDING
+    """Builds _ef_torch.so in-tree with g++ against the installed torch, again where that is another one."""
     import sysconfig
 
     import torch
     from torch.utils import cpp_extension
+    stamp, built_for = TORCH_BINDING + ".stamp", torch.__version__
+    if not force and os.path.exists(TORCH_BINDING) and os.path.exists(stamp):
+        with open(stamp) as f:
+            same = f.read() == built_for
+        if same and os.path.getmtime(TORCH_BINDING) >= max(os.path.getmtime(p) for p in TORCH_SOURCES):
+            return TORCH_BINDING
     cuda = os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"]
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+           f'-DEF_TORCH_VERSION="{built_for}"']
     for inc in cpp_extension.include_paths() + [sysconfig.get_paths()["include"], cuda]:
         cmd += ["-isystem", inc]
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
@@ -71,6 +75,8 @@ def build_torch_binding(force: bool = False) -> str:
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("g++ failed:\n" + res.stdout + res.stderr)
+    with open(stamp, "w") as f:
+        f.write(built_for)
     return TORCH_BINDING
 
 

@@ -375,4 +375,11 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ef_torch", nullptr, -1, methods, 
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__ef_torch() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__ef_torch() {
+    PyObject* const m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "torch_version", EF_TORCH_VERSION) < 0) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}

@@ -41,6 +41,9 @@ def _native():
         except ImportError as e:
             raise OSError("_ef_torch.so is missing: build it with `python -m paper_1905_10936_b200.build` "
                           "(there is no fallback path)") from e
+        if _ef_torch.torch_version != torch.__version__:
+            raise OSError(f"_ef_torch.so was built against torch {_ef_torch.torch_version}, this is {torch.__version__}: "
+                          "build it again with `python -m paper_1905_10936_b200.build`")
         _ef_torch.bind(tuple(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _CALLS), ef.EFError)
         _module, _bound = _ef_torch, lib
     return _module

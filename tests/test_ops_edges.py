@@ -57,3 +57,21 @@ def test_a_stride_past_the_copy_engine_s_limit_goes_through_the_workspace():
     need = ef.ef_checkpoint_weight_grad_workspace_bytes
     assert need(1, 1, 128, 128, BUF, (1 << 39) - 8) == 0
     assert need(1, 1, 128, 128, BUF, 1 << 39) >= 64 * 128 * 2
+
+
+def test_the_native_half_belongs_to_one_torch(monkeypatch):
+    """Built again where another torch is installed, and refused if it was not."""
+    class Compiled(Exception):
+        pass
+
+    def run(*args, **kwargs):
+        raise Compiled
+
+    monkeypatch.setattr(efbuild.subprocess, "run", run)
+    assert efbuild.build_torch_binding() == efbuild.TORCH_BINDING              # up to date: nothing is compiled
+    monkeypatch.setattr(torch, "__version__", "0.0.0")
+    with pytest.raises(Compiled):
+        efbuild.build_torch_binding()
+    monkeypatch.setattr(ops, "_bound", None)
+    with pytest.raises(OSError, match="built against torch"):
+        ops.checkpoint_load(host_checkpoint(1, 8))
