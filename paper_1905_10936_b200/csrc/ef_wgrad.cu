@@ -451,8 +451,9 @@ __global__ void __launch_bounds__(256) ef_wgrad_join_kernel(const float* __restr
         if (j0 + 256 * i < J) o[j0 + 256 * i] = accumulate ? o[j0 + 256 * i] + v[i] : v[i];
 }
 
-// dY as `terms` stacked bf16 matrices [terms * rows_pad][pitch] whose sum it is; rows and columns
-// past the end are 0.  A warp per 256-column segment.
+// dY as `terms` stacked bf16 matrices [terms * rows_pad][pitch] whose sum it is, the smallest first (the running sum is cut at
+// each step: small terms on top of a large sum put 64 fp32 tokens 3.9e-7 off in the 2-norm, below it 5.7e-8); rows and
+// columns past the end are 0.  A warp per 256-column segment.
 template <class T, bool ALIGNED, int TERMS>
 __global__ void __launch_bounds__(256) ef_wgrad_terms_kernel(const T* __restrict__ dy, long long ld, long long n, int J,
                                                              long long rows_pad, int pitch, __nv_bfloat16* __restrict__ out) {
@@ -471,7 +472,7 @@ __global__ void __launch_bounds__(256) ef_wgrad_terms_kernel(const T* __restrict
     float* const f = reinterpret_cast<float*>(v);
 #pragma unroll
     for (int t = 0; t < TERMS; ++t) {
-        __nv_bfloat16* const o = out + (t * rows_pad + row) * pitch;
+        __nv_bfloat16* const o = out + ((TERMS - 1 - t) * rows_pad + row) * pitch;
         __align__(16) __nv_bfloat16 h[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {

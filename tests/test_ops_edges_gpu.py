@@ -147,6 +147,16 @@ def test_weight_gradients_whose_waits_run_out_are_nan(n, c, j, dtype, wait_limit
     assert torch.equal(ops.checkpoint_weight_grad(kept, dy), good)
 
 
+@pytest.mark.parametrize("n", [16, 64, 576, 2085])
+def test_weight_grad_of_few_fp32_gradients_is_as_near_as_an_fp32_product(n):
+    """2-norm distance from 64 bits, next to that of the same product in fp32, whose sums are rounded at each step."""
+    kept, dy = ops.checkpoint_save(randn(1, n, 256)), randn(2, n, 200)
+    x = values_of(kept)
+    want, plain = x.t() @ dy.to(F8), x.float().t() @ dy
+    got = ops.checkpoint_weight_grad(kept, dy)
+    assert float((got.to(F8) - want).norm()) <= float((plain.to(F8) - want).norm())
+
+
 # ---- checkpoints -----------------------------------------------------------------------------
 def test_fp16_values_stay_finite_in_a_checkpoint():
     """Every finite fp16 value next to any other: what the checkpoint stands for is finite in fp16, at most one step off where
