@@ -10,7 +10,9 @@ import torch
 from paper_1905_10936_b200 import binding as ef
 from paper_1905_10936_b200 import build as efbuild
 from paper_1905_10936_b200 import ops
-from test_ops_gpu import EPS, F8, TYPES, act64, gen, ids, policy64, policy_case, quantised, randn, slope64, strided, values_of, within
+from test_ops_gpu import (EPS, F8, TYPES, U, act64, check_policy, gen, ids, policy64, policy_case, quantised, randn, rounded, slope64,
+                          strided, values_of, within)
+
 
 pytestmark = pytest.mark.gpu
 
@@ -129,6 +131,44 @@ def test_policy_rows_whose_waits_run_out_are_nan(n, c, dtype, wait_limit):
         assert torch.equal(again.logp, good.logp) and torch.equal(again.loss, good.loss)
 
 
+@pytest.mark.parametrize("c,dtype", [(12288, torch.bfloat16), (12289, torch.bfloat16), (6144, torch.float32), (6145, torch.float32),
+                                     (53248, torch.bfloat16), (53249, torch.bfloat16), (26624, torch.float32), (26625, torch.float32),
+                                     (53248, torch.float16)], ids=str)
+def test_policy_loss_on_both_sides_of_the_many_rows_borders(c, dtype):
+    """Enough rows for the kernels of four warps and of resident CTAs to be chosen, up to the widest row of which two share an
+    SM, and the next wider one.  logp's bound: its own rounding (u |logp|), the target's distance from the maximum (u of it), 4 u
+    for the exponentials' approximation and 2 u for their sum."""
+    n = 310
+    x, t, old, adv, w, ref = policy_case(c, n, c, dtype)
+    e = policy64(x, t, old, adv, w, ref, 0.2, 0.28, 0.04, 1.0)
+    e["t"] = t
+    depth = e["x"].amax(dim=1) - e["x"].gather(1, t[:, None]).view(n)
+    for view in (x, strided(x, 3, 1)):
+        for place in (False, True):
+            xv = strided(x, 3, 1) if place and view is not x else x.clone()
+            out = ops.policy_loss(xv, t, old, adv, w, ref_logp=ref, clip_low=0.2, clip_high=0.28, beta=0.04, in_place=place)
+            check_policy(out, e, dtype, 0.04, 1.0, adv, old, ref)
+            within(out.logp, e["logp"], U * (e["lp"].abs() + depth + 6.0), "logp")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=ids)
+def test_log_probabilities_and_loss_of_a_whole_vocabulary(dtype):
+    """50257 logits, many rows and few.  logp as above.  A token's loss before its own rounding is off by that of the ratio's
+    exponent (as logp, without the rounding of logp itself: 6 u and the distance), of expf (4 u) and six more roundings, times ratio
+    and advantage; the KL term's slope is below 0.1; the clipped side has three roundings and its own size."""
+    n, c = 600, 50257
+    x, t, old, adv, w, ref = policy_case(7, n, c, dtype)
+    e = policy64(x, t, old, adv, w, ref, 0.2, 0.2, 0.04, 1.0)
+    depth = e["x"].amax(dim=1) - e["x"].gather(1, t[:, None]).view(n)
+    for rows in (n, 40):
+        within(ops.token_logprob(x[:rows], t[:rows]), e["lp"][:rows], (U * (e["lp"].abs() + depth + 6.0))[:rows], "logp")
+    out = ops.policy_loss(x, t, old, adv, w, ref_logp=ref, beta=0.04)
+    off = U * (depth + 16.0) * (e["straight"].abs() + 0.1) * w.to(F8) + 4 * U * e["tok"].abs()
+    within(out.token_loss, e["tok"], off, "token loss")
+    total = e["tok"].sum()
+    within(out.loss[None], total[None], off.sum() + U * total.abs(), "loss")
+
+
 # ---- weight gradient -------------------------------------------------------------------------
 @pytest.mark.parametrize("n,c,j,dtype", [(65, 129, 257, torch.bfloat16), (2085, 1001, 777, torch.float32), (8192, 512, 1024, torch.bfloat16),
                                          (1500, 300, 100, torch.float16)], ids=str)
@@ -155,6 +195,17 @@ def test_weight_grad_of_few_fp32_gradients_is_as_near_as_an_fp32_product(n):
     want, plain = x.t() @ dy.to(F8), x.float().t() @ dy
     got = ops.checkpoint_weight_grad(kept, dy)
     assert float((got.to(F8) - want).norm()) <= float((plain.to(F8) - want).norm())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("n,c,j", [(8192, 384, 640), (9000, 1000, 130)])
+def test_weight_grad_keeps_the_precision_of_an_fp32_product(n, c, j, dtype):
+    """The tensor core cuts its running sum, so one accumulator over all tokens is 4e-6 off in the 2-norm and grows with their
+    number; in spans of 18 stages that are added up in registers the error is that of an fp32 product, 3e-7, twice of which is allowed."""
+    kept, dy = ops.checkpoint_save(randn(1, n, c)), randn(2, n, j, dtype=dtype)
+    want = values_of(kept).t() @ dy.to(F8)
+    got = ops.checkpoint_weight_grad(kept, dy)
+    assert float((got.to(F8) - want).norm()) <= 6e-7 * float(want.norm())
 
 
 # ---- checkpoints -----------------------------------------------------------------------------
@@ -282,6 +333,34 @@ def test_norm_rstd_is_rounded_once(c):
     want = 1.0 / torch.sqrt((x.to(F8) ** 2).mean(dim=1) + float(torch.tensor(EPS)))
     assert float((x.to(F8) ** 2).sum(dim=1).max()) < 2.0 ** 24
     assert torch.equal(ops.rmsnorm_forward(x, torch.ones(c, device="cuda"), EPS).rstd, want.float())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("c", [513, 600, 768, 1025, 1280, 1536, 2049, 2560, 2900, 5120, 6144, 6145])
+def test_norm_of_rows_between_the_powers_of_two(c, dtype):
+    """Rows of 3, 6, 12 and 24 warps, and of 12 warps with two segments each (fp32), have launch shapes of their own.  Bounds as
+    in the tests of the other widths: an error of (n + 64) u of the summed magnitudes for dw, of 84 u for dx, 48 u for y."""
+    for n in (1, 700):
+        x, r = randn(c, n, c, dtype=dtype, scale=2.0), randn(c + 1, n, c, dtype=dtype)
+        dy, dh, w = randn(c + 2, n, c, dtype=dtype), randn(c + 3, n, c, dtype=dtype), 1.0 + 0.2 * randn(c + 4, c)
+        for view in (lambda t: t, lambda t: strided(t, 5, 3)):
+            out = ops.rmsnorm_forward(view(x), w, EPS, residual=view(r), checkpoint=True)
+            h = x.to(F8) + r.to(F8)
+            rstd = 1.0 / torch.sqrt((h * h).mean(dim=1) + EPS)
+            y = h * rstd[:, None] * w.to(F8)
+            within(out.h, h, rounded(h, dtype, U * h.abs()), "h")
+            within(out.rstd, rstd, 48 * U * rstd, "rstd")
+            step = out.checkpoint.scales.to(F8).repeat_interleave(128, dim=1)[:, :c]
+            within(values_of(out.checkpoint), y, 0.5 * step + 96 * U * y.abs(), "codes")
+            kept = ops.checkpoint_save(x)
+            for source, hv in ((view(x), x.to(F8)), (kept, values_of(kept))):
+                got, got_w = ops.rmsnorm_backward(view(dy), source, w, out.rstd, dh=view(dh))
+                nh, uv = hv * out.rstd.to(F8)[:, None], dy.to(F8) * w.to(F8)
+                dot = (uv * nh).mean(dim=1, keepdim=True)
+                dx = out.rstd.to(F8)[:, None] * (uv - nh * dot) + dh.to(F8)
+                size = out.rstd.to(F8)[:, None] * (uv.abs() + nh.abs() * (uv * nh).abs().mean(dim=1, keepdim=True))
+                within(got, dx, rounded(dx, dtype, 84 * U * size + U * dh.to(F8).abs()), "dx")
+                within(got_w, (dy.to(F8) * nh).sum(dim=0), (n + 64) * U * (dy.to(F8) * nh).abs().sum(dim=0), "dw")
 
 
 # ---- tensors that torch differentiates -------------------------------------------------------
