@@ -226,7 +226,7 @@ int ef_set_state(ef_ctx* ctx, int32_t i, const float* momentum, const float* res
 int ef_step_count(ef_ctx* ctx, int64_t* t /* out: completed iterations */);
 
 /* Synchronises the context's stream and reads the device status word that kernels set when a
- * bounded device-side wait runs out (only the bulk-staged server kernel waits at all: on an
+ * bounded device-side wait runs out (of a context's kernels only the bulk-staged server kernel waits at all: on an
  * mbarrier that counts the bytes of its own copies, with an iteration limit).  Returns EF_OK,
  * EF_ERR_TIMEOUT (the results of the affected call are undefined; the word is cleared) or
  * EF_ERR_CUDA.  The step calls themselves never synchronise, so a caller who wants the check
@@ -458,6 +458,7 @@ int ef_worker_step_noalloc(const float* grad, float* momentum, float* residual,
  *     rows and more, but for short rows of the policy loss; a stride of 2^31 elements and more, but for the policy
  *     loss and the weight gradient), WORKSPACE, ALIGNMENT (a pointer that is
  *     not aligned to its element, or codes not to 16 bytes), UNSUPPORTED_DEVICE, CUDA.
+ *   - waits on the device are bounded; one that runs out makes the rows or the part of dW concerned NaN.
  *   - kernels are launched with programmatic stream serialization, wait on the device for the kernel before them on
  *     the stream, and do not signal early. */
 #define EF_TYPE_F32 0

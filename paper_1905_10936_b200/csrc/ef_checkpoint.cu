@@ -15,7 +15,7 @@
 // memory and no barrier.  8192 x 4096 bf16: GELU backward 33 us, 78 % of the copy rate; forward with
 // both checkpoints 42 us, 75 %: the two quantisations and the activation take 240 instructions per segment and issue
 // is 71 % busy.  Rows that do not allow 16-byte accesses (4099 x 2731 fp16, SwiGLU backward: 28 us, 48 %) are
-// bound by the number of accesses.
+// bound by the number of accesses: one per element and code.
 #include "ef_rows.cuh"
 
 #include <algorithm>

@@ -20,9 +20,10 @@
 //     shared memory.  (Clusters of four 25 KB slices for 50257 bf16 logits, the same memory per SM, took
 //     188 us instead of 145 at 4096 rows: they start and end together.)
 //   - short rows: 1 or 4 warps, which walk over rows and load the next one while they work on this one
-//     (16000 x 1001 bf16: 27 us; as rows of their own CTA 74).
-// 4096 x 50257 bf16, 15 % of the rows masked: 137 us for 762 MB, 85 % of the copy rate; two rows of 98 KB on an SM do not
+//     (16000 x 1001 bf16: 28 us; as rows of their own CTA 74; floor 9).  What bounds them is the chain of each row, with few in flight.
+// 4096 x 50257 bf16, 15 % of the rows masked: 138 us for 762 MB, 84 % of the copy rate; two rows of 98 KB on an SM do not
 // always cover one another's sums (8192 x 32000, three rows: 91 %).
+// A device-side wait that runs out is the last of its CTA (or thread): copies in flight land, and rows not finished become NaN.
 #include "ef_rows.cuh"
 
 #include <algorithm>
@@ -411,7 +412,7 @@ __global__ void __launch_bounds__(Shape<GW>::kBlock, Shape<GW>::kCtas) ef_policy
 // reads and writes of HBM run side by side inside each CTA.  It also fetches the row's scalars and ends, which cost the
 // others two dependent accesses.  The next row is the one of a CTA of the grid that has not started yet and now
 // never will (cluster launch control), so masked rows leave no CTA idle.
-// 4096 x 50257 bf16, 15 % masked: 137 us, one row per CTA 151; 8192 x 32000: 162 and 180 us; 8192 x 16001 fp16: 96 and 114.
+// 4096 x 50257 bf16, 15 % masked: 138 us, one row per CTA 151; 8192 x 32000: 163 and 180 us; 8192 x 16001 fp16: 97 and 114.
 // Four chunks per row took 139 us and seven 146: each costs a wait.  Sixteen warps: 146.
 __device__ __forceinline__ void ask_for_cta(uint4* answer, unsigned long long* bar) {
     efk::mbar_expect_tx(bar, 16);
@@ -766,7 +767,8 @@ int launch(int32_t type, PolicyArgs& a, cudaStream_t st) {
         const int64_t bytes = (int64_t)a.C * (int64_t)sizeof(T);
         if (bytes <= kShortBytes[0]) return launch_policy<T, 1>(a, st);
         if (bytes <= kShortBytes[1] && a.n > 2 * efh::kSMs) return launch_policy<T, 4>(a, st);
-        // up to two rows per SM there is no next row to load early (300 x 50257 bf16: 19.4 us here, 19.7 there)
+        // Up to two rows per SM there is no next row to load early (300 x 50257 bf16: resident CTAs 20 us, a CTA per row 19.7).
+        // With few rows more a CTA per row is still ahead (400 x 50257: 26.8 and 29.2 us, 900 x 20001: 22.9 and 26.0), with many far behind.
         if (bytes <= kAloneBytes && a.n > 2 * efh::kSMs && a.n <= 0x7fffffff) return launch_rows<T>(a, st);
         return launch_policy<T, kLongWarps>(a, st);
     });

@@ -16,15 +16,18 @@
 // The tensor core cuts its running sum at each step instead of rounding it: after 8192 tokens in one
 // accumulator dW was 4.3e-6 off (2-norm), ten times an fp32 product.  So an accumulator runs over
 // kSpan stages only; there are two, and while one runs the convert warps add the other into fp32
-// registers: 2.1e-7 off, an fp32 product 2.9e-7.
+// registers: 2.1e-7 off (8192 x 384 x 640; fp32 products of the same 1e-7 to 5e-7).
 //
-// 8192 tokens, 1024 x 4096: 60 us, 1140 TFLOP/s; cuBLAS on operands that are bf16 already 45 us.  What bounds it is the
+// 8192 tokens, 1024 x 4096: 60 to 61 us, 1130 TFLOP/s; cuBLAS on operands that are bf16 already 45 us.  What bounds it is the
 // convert warps' work beside the matrix instructions (without the conversion 52 us; 16 times 128 x 256
 // sums in 64 registers each leave them 96 registers at 18 warps).  Steps on the way: CTAs by themselves, 128 x 256,
 // 120 us; pairs, with a release at cluster scope for each stage of the second CTA, 149, without it
-// 107; one issuing thread whose operands the compiler moved to uniform registers at every
-// instruction, 75, the whole warp together, 68; codes read from global memory by the convert warps, whose
+// 107; a single lane that walks the
+// issuing loop, 75, the whole warp together with one elected lane, 68; codes read from global memory by the convert warps, whose
 // fence before each hand-over waits for loads under way, 68 to 72, by TMA and scales in batches, 60.
+//
+// Device-side waits are bounded and have one answer per warp.  One that runs out makes the tile NaN; the load warp waits for its
+// copies, and the issuing warp for its matrix instructions, before the pair parts and frees its accumulators.
 //
 // dY of 16-byte aligned bf16 rows is read as it is.  Other types and strides are first rewritten
 // as bf16 rows in the workspace: fp16 as the sum of two bf16 values (exact: 11 bits), fp32 as the sum of
@@ -390,8 +393,7 @@ ef_wgrad_kernel(const WgradArgs a, const __grid_constant__ CUtensorMap codes, co
         const unsigned tmem = __shfl_sync(kFull, s_tmem, 0);
         cluster_wait();
         // One thread's latency per stage bounds the pair.  The warp stays together and its values are
-        // the same for all lanes, one elected thread issues: with a single lane walking the loop
-        // the compiler moved every operand into uniform registers anew, 950 clocks a stage.
+        // the same for all lanes, one elected thread issues (68 us; a single lane walking the loop 75).
         const bool one = elect_one();
         const unsigned long long first = operand(efk::smem_u32(stage0));
         int s = 0, at = 0, span = 0;             // at: stage of the span
